@@ -244,6 +244,94 @@ fp2_status fp2_read_status(fp2_plan* plan, void* workspace, int32_t* h_status_wo
  * the same plan and workspace are unaffected.  Nothing is allocated; one kernel on `stream`. */
 fp2_status fp2_selftest_bounded_wait(fp2_plan* plan, void* workspace, fp2_stream stream);
 
+/* ------------------------------------------------------------------------------------------------------------
+ * The cache itself: filling it, reading it back, decoding from it.  (No counterpart in the paper, which leaves the cache and
+ * the decode phase to the serving engine, Sec. 3.4.)
+ *
+ * An fp2_cache describes a paged cache: shapes and what its pages hold.  It is made once; the calls below read the lengths of
+ * the sequences on the DEVICE, so a captured CUDA graph stays valid while sequences grow, and they allocate nothing, copy
+ * nothing and do not synchronise.  A handle does not change after its creation: calls on it may run in several threads and on
+ * several streams, each stream with a workspace of its own (two calls whose kernels may overlap must not share one).
+ *
+ * What the pages hold (fp2_cache_format).  k_cache, v_cache: [num_pages, page_size, num_kv_heads, 128], as for the stage calls.
+ *   FP2_CACHE_BF16      BF16; no scales (NULL).  What a BF16 plan reads.
+ *   FP2_CACHE_FP8_HEAD  e4m3, k_scale / v_scale fp32 [num_kv_heads], given by the caller.  What an FP8 plan reads.
+ *   FP2_CACHE_FP8_PAGE  e4m3, k_scale / v_scale fp32 [num_pages, num_kv_heads]: a scale per page and KV head, which
+ *                       fp2_cache_append chooses.  fp2_decode reads it; the stage calls read it after fp2_cache_expand.
+ * Scales are positive and finite.  Page ids, positions and masks are those of the stage calls: query i of a sequence with Lq
+ * new and L tokens in all sits at position L - Lq + i.
+ *
+ * Lengths on the device that do not fit -- offsets that fall or pass the number of rows, more tokens than max_pages_per_seq
+ * pages hold -- make the calls leave that sequence out; a page id outside [0, num_pages) leaves out the tokens of that page.
+ * Both are recorded in the workspace's status block (fp2_cache_read_status). */
+typedef enum { FP2_CACHE_BF16 = 0, FP2_CACHE_FP8_HEAD = 1, FP2_CACHE_FP8_PAGE = 2 } fp2_cache_format;
+
+typedef struct fp2_cache fp2_cache; /* opaque */
+
+typedef struct {
+  int32_t max_seqs;       /* most sequences of a call                                                 */
+  int32_t num_q_heads, num_kv_heads;
+  int32_t head_dim;       /* must be 128                                                              */
+  int32_t page_size;      /* 8, 16, 32, 64 or 128                                                     */
+  int32_t num_pages, max_pages_per_seq;
+  int32_t format;         /* fp2_cache_format                                                         */
+  float softmax_scale;    /* 0 selects 1 / sqrt(head_dim)                                             */
+} fp2_cache_params;
+
+/* Host only; FP2_ERR_INVALID_ARG / _UNSUPPORTED / _CAPACITY (a sequence of more than 2^30 tokens) for shapes that are not
+ * handled.  Without a usable CUDA device the handle is returned, but calls on it return FP2_ERR_CUDA. */
+fp2_status fp2_cache_create(const fp2_cache_params* params, fp2_cache** out);
+void fp2_cache_destroy(fp2_cache* cache);
+
+/* Bytes of device workspace of the calls below: 1024-byte aligned, zeroed once by the caller before the first call. */
+fp2_status fp2_cache_sizes(const fp2_cache* cache, int64_t* workspace_bytes);
+
+/* Writes the keys and values of new tokens into their pages.
+ *   k_new, v_new   BF16 [total_new, num_kv_heads, 128], `new_stride` elements from token to token (a multiple of 8, at least
+ *                  num_kv_heads * 128: slices of a fused projection's output), 16-byte aligned
+ *   cu_seqlens_new int32 [num_seqs + 1]; seqlens_k int32 [num_seqs]: tokens in the cache AFTER the call
+ * Token i of the n new ones of a sequence goes to position seqlens_k - n + i.  BF16 caches take a copy; 8-bit ones
+ * e4m3(x / scale), nearest even, saturating at +-448 (infinities too; NaN stays NaN), where the scale is
+ *   FP8_HEAD: the caller's;
+ *   FP8_PAGE: the smallest power of two that leaves the largest finite magnitude among the page's new tokens (of that KV head)
+ *             at 448 or less, not below 2^-100; where the page holds earlier tokens of the sequence, not below its present
+ *             scale either, and if that has to grow the earlier tokens are rounded to the new one.  Written to k_scale / v_scale.
+ * Rows of a page behind the last token, and pages without new tokens, are left as they are.  A page that new tokens of two
+ * sequences go to is not allowed (a shared prefix ends with a full page).  One kernel on `stream`. */
+fp2_status fp2_cache_append(const fp2_cache* cache, const void* k_new, const void* v_new, int64_t new_stride,
+                            const int32_t* page_table, const int32_t* cu_seqlens_new, const int32_t* seqlens_k,
+                            int32_t num_seqs, int32_t total_new, void* k_cache, void* v_cache, float* k_scale,
+                            float* v_scale, void* workspace, fp2_stream stream);
+
+/* An 8-bit cache as BF16 pages (code times scale, rounded once), for stage calls of a BF16 plan: prefill chunks behind a
+ * prefix that is kept in 8 bits, or block selection on it.  Page j of sequence b goes to page out_page_table[b][j] of k_out /
+ * v_out, BF16 [out_num_pages, page_size, num_kv_heads, 128], 16-byte aligned; out_page_table has the shape of page_table, and
+ * no page may occur in it twice.  Rows of a last page behind the sequence's end become zero.  FP2_ERR_UNSUPPORTED for BF16
+ * caches.  One kernel on `stream`. */
+fp2_status fp2_cache_expand(const fp2_cache* cache, const void* k_cache, const void* v_cache, const int32_t* page_table,
+                            const int32_t* seqlens_k, int32_t num_seqs, const float* k_scale, const float* v_scale,
+                            void* k_out, void* v_out, const int32_t* out_page_table, int32_t out_num_pages,
+                            void* workspace, fp2_stream stream);
+
+/* Attention of the newest tokens of every sequence over its pages: one token each, or a few (drafts, short turns; any number
+ * works, but prompts belong to the prefill calls, whose tiles are made for them).  The new tokens' own keys and values are in
+ * the cache (fp2_cache_append comes first).  Key j is visible to a query at position p iff
+ *     j <= p  and  (window_tokens == 0  or  p - j < window_tokens  or  j < sink_tokens).
+ *   q   BF16 [total_q, num_q_heads, 128], `q_stride` elements from token to token (a multiple of 8), 16-byte aligned
+ *   out BF16 [total_q, num_q_heads, 128], 16-byte aligned; lse fp32 [num_q_heads, total_q] or NULL, as for the stage calls
+ * Rows of out / lse behind cu_seqlens_q[num_seqs] are left as they are.  A query that sees nothing (position below 0, or all its
+ * pages missing) gets zeros and lse = -inf.  What stands in places that no query of its sequence sees never matters; a V row
+ * that some queries see must be finite for the others of the same call too.  The same call gives the same bits every time.
+ * One kernel on `stream`. */
+fp2_status fp2_decode(const fp2_cache* cache, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                      const int32_t* page_table, const int32_t* cu_seqlens_q, const int32_t* seqlens_k, int32_t num_seqs,
+                      int32_t total_q, const float* k_scale, const float* v_scale, int32_t window_tokens,
+                      int32_t sink_tokens, void* out, float* lse, void* workspace, fp2_stream stream);
+
+/* Synchronises `stream`, reads the status block of `workspace` and clears it.  FP2_ERR_INVALID_ARG if a page id was outside the
+ * pool (word 2, bit 1) or lengths did not fit (word 2, bit 2), else FP2_OK.  h_status_words: NULL or 8 words of host memory. */
+fp2_status fp2_cache_read_status(const fp2_cache* cache, void* workspace, int32_t* h_status_words, fp2_stream stream);
+
 /* Number of kernels the last stage call on this plan enqueued (host counter). */
 int32_t fp2_last_launch_count(const fp2_plan* plan);
 

@@ -21,7 +21,9 @@ EXPORTS = ["fp2_plan_create", "fp2_plan_sizes", "fp2_plan_destroy", "fp2_plan_se
            "fp2_pool_blocks",
            "fp2_sparse_prefill", "fp2_dense_prefill", "fp2_dense_prefill_static", "fp2_export_csr",
            "fp2_page_table_from_token_map", "fp2_plan_set_split", "fp2_pool_carry", "fp2_pool_carry_count",
-           "fp2_read_status", "fp2_selftest_bounded_wait", "fp2_last_launch_count", "fp2_status_string"]
+           "fp2_read_status", "fp2_selftest_bounded_wait", "fp2_last_launch_count", "fp2_status_string",
+           "fp2_cache_create", "fp2_cache_destroy", "fp2_cache_sizes", "fp2_cache_append", "fp2_cache_expand", "fp2_decode",
+           "fp2_cache_read_status"]
 
 
 class Fp2Error(RuntimeError):
@@ -35,6 +37,14 @@ class fp2_params(C.Structure):
                                          "block_size", "tile_rows", "page_size", "num_pages", "max_pages_per_seq",
                                          "sink_tokens", "window_tokens", "use_correction")] + \
                [("alpha", C.c_float), ("softmax_scale", C.c_float), ("dtype", C.c_int32)]
+
+
+CACHE_BF16, CACHE_FP8_HEAD, CACHE_FP8_PAGE = 0, 1, 2     # fp2_cache_format
+
+
+class fp2_cache_params(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("max_seqs", "num_q_heads", "num_kv_heads", "head_dim", "page_size", "num_pages",
+                                         "max_pages_per_seq", "format")] + [("softmax_scale", C.c_float)]
 
 
 _lib = None
@@ -94,6 +104,23 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.fp2_read_status.restype = C.c_int
     lib.fp2_last_launch_count.argtypes = [C.c_void_p]
     lib.fp2_last_launch_count.restype = C.c_int32
+    lib.fp2_cache_create.argtypes = [C.POINTER(fp2_cache_params), C.POINTER(C.c_void_p)]
+    lib.fp2_cache_create.restype = C.c_int
+    lib.fp2_cache_destroy.argtypes = [C.c_void_p]
+    lib.fp2_cache_destroy.restype = None
+    lib.fp2_cache_sizes.argtypes = [C.c_void_p, C.POINTER(C.c_int64)]
+    lib.fp2_cache_sizes.restype = C.c_int
+    lib.fp2_cache_append.argtypes = [C.c_void_p, vp, vp, C.c_int64, i32p, i32p, i32p, C.c_int32, C.c_int32, vp, vp, f32p, f32p,
+                                     vp, C.c_void_p]
+    lib.fp2_cache_append.restype = C.c_int
+    lib.fp2_cache_expand.argtypes = [C.c_void_p, vp, vp, i32p, i32p, C.c_int32, f32p, f32p, vp, vp, i32p, C.c_int32, vp,
+                                     C.c_void_p]
+    lib.fp2_cache_expand.restype = C.c_int
+    lib.fp2_decode.argtypes = [C.c_void_p, vp, C.c_int64, vp, vp, i32p, i32p, i32p, C.c_int32, C.c_int32, f32p, f32p, C.c_int32,
+                               C.c_int32, vp, f32p, vp, C.c_void_p]
+    lib.fp2_decode.restype = C.c_int
+    lib.fp2_cache_read_status.argtypes = [C.c_void_p, vp, C.POINTER(C.c_int32), C.c_void_p]
+    lib.fp2_cache_read_status.restype = C.c_int
     lib.fp2_status_string.argtypes = [C.c_int]
     lib.fp2_status_string.restype = C.c_char_p
     _lib = lib
@@ -258,6 +285,140 @@ def fp2_pool_carry(dst: Plan, dst_workspace, src: Plan, src_workspace, src_seq, 
 def fp2_selftest_bounded_wait(plan: Plan, workspace, stream=None):
     """Launches the library's bounded-wait probe: a wait that runs out, recorded in the status block of `workspace`."""
     _check(load().fp2_selftest_bounded_wait(plan.handle, _ptr(workspace), _stream(stream)), "fp2_selftest_bounded_wait")
+
+
+class Cache:
+    """Owner of an fp2_cache handle: the shapes and the format of a paged KV cache (host memory only)."""
+
+    def __init__(self, params: dict):
+        lib = load()
+        self.params = fp2_cache_params(**params)
+        h = C.c_void_p()
+        _check(lib.fp2_cache_create(C.byref(self.params), C.byref(h)), "fp2_cache_create")
+        self.handle = h
+        n = C.c_int64()
+        _check(lib.fp2_cache_sizes(h, C.byref(n)), "fp2_cache_sizes")
+        self.workspace_bytes = n.value
+        self._device = torch.device("cuda", torch.cuda.current_device()) if torch.cuda.is_available() else None
+        p = self.params
+        self._fp8 = p.format != CACHE_BF16
+        self._pool = (p.num_pages, p.page_size, p.num_kv_heads, p.head_dim)
+        self._scales = {CACHE_BF16: None, CACHE_FP8_HEAD: (p.num_kv_heads,), CACHE_FP8_PAGE: (p.num_pages, p.num_kv_heads)}[p.format]
+
+    def new_workspace(self, device="cuda") -> torch.Tensor:
+        """Zeroed device workspace, 1024-byte aligned (one per stream that runs calls at the same time)."""
+        raw = torch.zeros(self.workspace_bytes + 1024, dtype=torch.uint8, device=device)
+        shift = (-raw.data_ptr()) % 1024
+        ws = raw[shift:shift + self.workspace_bytes]
+        ws._fp2_keepalive = raw
+        return ws
+
+    def new_pages(self, device="cuda"):
+        """Zeroed k_cache, v_cache, k_scale, v_scale of the cache's shapes (scales one; None for BF16)."""
+        dt = torch.uint8 if self._fp8 else torch.bfloat16
+        k, v = (torch.zeros(self._pool, dtype=dt, device=device) for _ in "kv")
+        if self._scales is None:
+            return k, v, None, None
+        ks, vs = (torch.ones(self._scales, dtype=torch.float32, device=device) for _ in "kv")
+        return k, v, ks, vs
+
+    def _check_pages(self, where, device, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, num_seqs, workspace):
+        if self._device is not None and device != self._device:
+            raise Fp2Error(1, f"{where}: tensors on {device}, the cache was made for {self._device}")
+        kinds = _E4M3 if self._fp8 else _BF16
+        _want(where, device, k_cache, kinds, self._pool)
+        _want(where, device, v_cache, kinds, self._pool)
+        if self._scales is not None:
+            _want(where, device, k_scale, _F32, self._scales)
+            _want(where, device, v_scale, _F32, self._scales)
+        _want(where, device, page_table, _I32, (num_seqs, self.params.max_pages_per_seq))
+        _want(where, device, seqlens_k, _I32, (num_seqs,))
+        if workspace.numel() < self.workspace_bytes or workspace.device != device:
+            raise Fp2Error(1, f"{where}: workspace too small or on another device")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            load().fp2_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+_E4M3, _BF16, _F32, _I32 = (torch.uint8, torch.float8_e4m3fn), (torch.bfloat16,), (torch.float32,), (torch.int32,)
+
+
+def _want(where, device, t, dtypes, shape):
+    """The C ABI sees addresses only: what a tensor must be for the address to mean what the call takes it for."""
+    if t is None or t.dtype not in dtypes or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}"
+        raise Fp2Error(1, f"{where}: wanted contiguous {dtypes[0]} {shape} on {device}, got {got}")
+
+
+def _rows(where, device, t, heads):
+    """Token stride of a BF16 [tokens, heads, 128] tensor whose tokens may lie apart (a slice of a fused projection)."""
+    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[1:] != (heads, 128) or t.device != device or \
+            t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
+        raise Fp2Error(1, f"{where}: wanted BF16 [tokens, {heads}, 128] on {device}, heads next to each other, got {t.dtype} "
+                          f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else heads * 128
+
+
+def fp2_cache_append(cache: Cache, k_new, v_new, page_table, cu_seqlens_new, seqlens_k, k_cache, v_cache, k_scale, v_scale,
+                     workspace, stream=None):
+    """Writes the keys and values of new tokens into their pages (quantised where the cache holds 8 bits; FP8_PAGE caches get
+    the pages' scales too).  seqlens_k: tokens in the cache after the call."""
+    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_cache_append"
+    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    _want(where, dev, cu_seqlens_new, _I32, (ns + 1,))
+    heads = cache.params.num_kv_heads
+    stride = _rows(where, dev, k_new, heads)
+    if _rows(where, dev, v_new, heads) != stride or v_new.shape[0] != k_new.shape[0]:
+        raise Fp2Error(1, f"{where}: k_new and v_new differ in tokens or strides")
+    _check(load().fp2_cache_append(cache.handle, _ptr(k_new), _ptr(v_new), stride, _ptr(page_table), _ptr(cu_seqlens_new),
+                                   _ptr(seqlens_k), ns, k_new.shape[0], _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                   _ptr(v_scale), _ptr(workspace), _stream(stream)), where)
+
+
+def fp2_cache_expand(cache: Cache, k_cache, v_cache, page_table, seqlens_k, k_scale, v_scale, k_out, v_out, out_page_table,
+                     workspace, stream=None):
+    """An 8-bit cache as BF16 pages [out_num_pages, page_size, num_kv_heads, 128] for stage calls of a BF16 plan."""
+    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_cache_expand"
+    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    _want(where, dev, out_page_table, _I32, tuple(page_table.shape))
+    pool = (k_out.shape[0],) + cache._pool[1:]
+    _want(where, dev, k_out, _BF16, pool)
+    _want(where, dev, v_out, _BF16, pool)
+    _check(load().fp2_cache_expand(cache.handle, _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(seqlens_k), ns,
+                                   _ptr(k_scale), _ptr(v_scale), _ptr(k_out), _ptr(v_out), _ptr(out_page_table),
+                                   k_out.shape[0], _ptr(workspace), _stream(stream)), where)
+
+
+def fp2_decode(cache: Cache, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, k_scale, v_scale, out, lse, workspace,
+               window_tokens: int = 0, sink_tokens: int = 0, stream=None):
+    """Attention of the newest few tokens of every sequence over its pages, with an optional sliding window and sinks."""
+    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_decode"
+    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    _want(where, dev, cu_seqlens_q, _I32, (ns + 1,))
+    heads, total_q = cache.params.num_q_heads, q.shape[0]
+    stride = _rows(where, dev, q, heads)
+    _want(where, dev, out, _BF16, (total_q, heads, 128))
+    if lse is not None:
+        _want(where, dev, lse, _F32, (heads, total_q))
+    _check(load().fp2_decode(cache.handle, _ptr(q), stride, _ptr(k_cache), _ptr(v_cache), _ptr(page_table), _ptr(cu_seqlens_q),
+                             _ptr(seqlens_k), ns, total_q, _ptr(k_scale), _ptr(v_scale), window_tokens, sink_tokens, _ptr(out),
+                             _ptr(lse), _ptr(workspace), _stream(stream)), where)
+
+
+def fp2_cache_read_status(cache: Cache, workspace, stream=None, raise_on_error: bool = True):
+    words = (C.c_int32 * 8)()
+    code = load().fp2_cache_read_status(cache.handle, _ptr(workspace), words, _stream(stream))
+    if raise_on_error:
+        _check(code, f"fp2_cache_read_status words={list(words)}")
+    return code, list(words)
 
 
 def fp2_read_status(plan: Plan, workspace, stream=None, raise_on_error: bool = True):

@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfp2.so")
-SOURCES = [os.path.join(CSRC, "fp2_api.cu")]
+SOURCES = [os.path.join(CSRC, "fp2_api.cu"), os.path.join(CSRC, "fp2_cache_api.cu")]
 
 
 def _deps():
@@ -33,7 +33,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
-           "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-o", LIB] + SOURCES
+           "-shared", "-Xcompiler", "-fPIC", "-Xptxas", "-v", "-t", "2", "-o", LIB] + SOURCES
     res = subprocess.run(cmd, capture_output=True, text=True)
     if verbose or res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)

@@ -1,0 +1,133 @@
+"""The paged KV cache on the host: what its calls refuse, before anything is launched."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2608_19758_b200 import binding
+
+
+def cache_params(**kw):
+    p = dict(max_seqs=4, num_q_heads=8, num_kv_heads=2, head_dim=128, page_size=16, num_pages=64, max_pages_per_seq=32,
+             format=2, softmax_scale=0.0)
+    p.update(kw)
+    return p
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(head_dim=64), 2), (dict(page_size=48), 2), (dict(page_size=4), 2), (dict(page_size=256), 2), (dict(page_size=0), 2),
+    (dict(format=3), 2), (dict(format=-1), 2), (dict(num_q_heads=7), 1), (dict(num_q_heads=0), 1), (dict(num_kv_heads=0), 1),
+    (dict(max_seqs=0), 1), (dict(num_pages=0), 1), (dict(max_pages_per_seq=0), 1), (dict(softmax_scale=-1.0), 1),
+    (dict(softmax_scale=float("nan")), 1), (dict(softmax_scale=float("inf")), 1), (dict(max_pages_per_seq=(1 << 26) + 1), 3),
+    (dict(num_q_heads=1 << 14, num_kv_heads=1 << 14), 3),
+])
+def test_cache_create_refuses(kw, code):
+    with pytest.raises(binding.Fp2Error) as e:
+        binding.Cache(cache_params(**kw))
+    assert e.value.code == code
+
+
+def test_null_handles_and_pointers():
+    lib = binding.load()
+    assert lib.fp2_cache_create(None, None) == 1
+    assert lib.fp2_cache_sizes(None, None) == 1
+    lib.fp2_cache_destroy(None)
+    p = C.c_void_p(4096)
+    assert lib.fp2_cache_append(None, p, p, 256, p, p, p, 1, 1, p, p, p, p, p, None) == 1
+    assert lib.fp2_cache_expand(None, p, p, p, p, 1, p, p, p, p, p, 1, p, None) == 1
+    assert lib.fp2_decode(None, p, 1024, p, p, p, p, p, 1, 1, p, p, 0, 0, p, None, p, None) == 1
+    assert lib.fp2_cache_read_status(None, p, None, None) == 1
+
+
+def _append(lib, h, **kw):
+    a = dict(k_new=4096, v_new=4096, stride=256, pt=4096, cu=4096, lk=4096, ns=2, total=3, k=4096, v=4096, ks=4096, vs=4096, ws=4096)
+    a.update(kw)
+    return lib.fp2_cache_append(h, a["k_new"], a["v_new"], a["stride"], a["pt"], a["cu"], a["lk"], a["ns"], a["total"], a["k"],
+                                a["v"], a["ks"], a["vs"], a["ws"], None)
+
+
+def _expand(lib, h, **kw):
+    a = dict(k=4096, v=4096, pt=4096, lk=4096, ns=2, ks=4096, vs=4096, ko=4096, vo=4096, opt=4096, pages=8, ws=4096)
+    a.update(kw)
+    return lib.fp2_cache_expand(h, a["k"], a["v"], a["pt"], a["lk"], a["ns"], a["ks"], a["vs"], a["ko"], a["vo"], a["opt"],
+                                a["pages"], a["ws"], None)
+
+
+def _decode(lib, h, **kw):
+    a = dict(q=4096, stride=1024, k=4096, v=4096, pt=4096, cu=4096, lk=4096, ns=2, total=3, ks=4096, vs=4096, w=0, s=0, out=4096,
+             lse=None, ws=4096)
+    a.update(kw)
+    return lib.fp2_decode(h, a["q"], a["stride"], a["k"], a["v"], a["pt"], a["cu"], a["lk"], a["ns"], a["total"], a["ks"],
+                          a["vs"], a["w"], a["s"], a["out"], a["lse"], a["ws"], None)
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_calls_refuse_bad_arguments_before_they_look_for_a_device(fmt):
+    """(Made-up addresses: only where there is no device, so that the good call ends with FP2_ERR_CUDA.)"""
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    lib = binding.load()
+    cache = binding.Cache(cache_params(format=fmt))
+    h = cache.handle
+    common = [dict(k=None), dict(v=None), dict(k=4104), dict(v=4104), dict(pt=None), dict(lk=None), dict(ws=None), dict(ws=4096 + 512),
+              dict(ns=-1), dict(ns=5)]
+    if fmt:
+        common += [dict(ks=None), dict(vs=None)]
+    assert _append(lib, h) == 4 and _decode(lib, h) == 4
+    if not fmt:
+        assert _append(lib, h, ks=None, vs=None) == 4 and _decode(lib, h, ks=None, vs=None) == 4
+    for kw in common + [dict(k_new=None), dict(v_new=None), dict(k_new=4104), dict(v_new=4104), dict(cu=None), dict(total=-1),
+                        dict(stride=255), dict(stride=260), dict(stride=128), dict(stride=-256)]:
+        assert _append(lib, h, **kw) == 1, kw
+    for kw in common + [dict(q=None), dict(q=4104), dict(out=None), dict(out=4104), dict(cu=None), dict(total=-1), dict(w=-1),
+                        dict(s=-1), dict(stride=1023), dict(stride=1020), dict(stride=512), dict(stride=-1024)]:
+        assert _decode(lib, h, **kw) == 1, kw
+    assert _decode(lib, h, total=(1 << 31) - 1) == 3
+    if fmt == 0:
+        assert _expand(lib, h) == 2      # BF16 pages already
+    else:
+        assert _expand(lib, h) == 4
+        for kw in common + [dict(ko=None), dict(vo=None), dict(ko=4104), dict(vo=4104), dict(opt=None), dict(pages=-1)]:
+            assert _expand(lib, h, **kw) == 1, kw
+    # nothing to do: fine without a device, and without data
+    assert _append(lib, h, total=0, k_new=None, v_new=None) == 0 and _append(lib, h, ns=0) == 0
+    assert _decode(lib, h, total=0, q=None, out=None) == 0 and _decode(lib, h, ns=0) == 0
+    assert lib.fp2_cache_read_status(h, 4096, None, None) == 4
+    cache.close()
+
+
+def test_binding_refuses_tensors_that_are_not_what_the_address_is_taken_for():
+    """Types, shapes, strides and devices are checked where the tensors are still known; nothing is launched."""
+    cache = binding.Cache(cache_params(max_seqs=3))
+    k, v, ks, vs = cache.new_pages("cpu")
+    ws = cache.new_workspace("cpu")
+    pt = torch.zeros(3, 32, dtype=torch.int32)
+    cu, lk = torch.tensor([0, 1, 2, 3], dtype=torch.int32), torch.tensor([5, 6, 7], dtype=torch.int32)
+    q = torch.zeros(3, 8, 128, dtype=torch.bfloat16)
+    new = torch.zeros(3, 2, 128, dtype=torch.bfloat16)
+    good = dict(q=q, k_cache=k, v_cache=v, page_table=pt, cu_seqlens_q=cu, seqlens_k=lk, k_scale=ks, v_scale=vs,
+                out=torch.zeros_like(q), lse=torch.zeros(8, 3), workspace=ws)
+    for name, bad in [("q", q.float()), ("q", q.transpose(0, 1)), ("q", torch.zeros(3, 8, 256, dtype=torch.bfloat16)[:, :, ::2]),
+                      ("q", torch.zeros(3, 4, 128, dtype=torch.bfloat16)), ("k_cache", k.to(torch.bfloat16)), ("v_cache", v[:5]),
+                      ("page_table", pt.long()), ("page_table", pt[:, :16]), ("cu_seqlens_q", cu[:3]), ("seqlens_k", lk.long()),
+                      ("k_scale", ks[0]), ("k_scale", None), ("v_scale", vs.double()), ("out", torch.zeros(2, 8, 128, dtype=torch.bfloat16)),
+                      ("out", q.float()), ("lse", torch.zeros(3, 8)), ("workspace", ws[:100])]:
+        with pytest.raises(binding.Fp2Error) as e:
+            binding.fp2_decode(cache, **{**good, name: bad})
+        assert e.value.code == 1, name
+    good = dict(k_new=new, v_new=new, page_table=pt, cu_seqlens_new=cu, seqlens_k=lk, k_cache=k, v_cache=v, k_scale=ks, v_scale=vs,
+                workspace=ws)
+    wide = torch.zeros(3, 4, 128, dtype=torch.bfloat16)
+    for name, bad in [("k_new", new.half()), ("k_new", wide[:, ::2]), ("v_new", wide[:, :2]), ("v_new", new[:2]),
+                      ("cu_seqlens_new", cu.long()), ("k_cache", k.view(-1, 16, 2, 64))]:
+        with pytest.raises(binding.Fp2Error) as e:
+            binding.fp2_cache_append(cache, **{**good, name: bad})
+        assert e.value.code == 1, name
+    out = torch.zeros(9, 16, 2, 128, dtype=torch.bfloat16)
+    good = dict(k_cache=k, v_cache=v, page_table=pt, seqlens_k=lk, k_scale=ks, v_scale=vs, k_out=out, v_out=out.clone(),
+                out_page_table=pt, workspace=ws)
+    for name, bad in [("k_out", out.float()), ("v_out", out[:4]), ("out_page_table", pt[:2]), ("k_out", out[:, :8])]:
+        with pytest.raises(binding.Fp2Error) as e:
+            binding.fp2_cache_expand(cache, **{**good, name: bad})
+        assert e.value.code == 1, name
+    cache.close()
