@@ -149,6 +149,20 @@ fp2_status fp2_dense_prefill(fp2_plan* plan, const void* q, const void* k_cache,
                              const float* q_scale, const float* k_scale, const float* v_scale, void* out,
                              float* lse, void* workspace, fp2_stream stream);
 
+/* (No counterpart in the paper, whose sink and window sets force whole blocks into a list.)  Local causal attention, token
+ * exact: key j is visible to a query at position p iff  j <= p  and  (p - j < window_tokens  or  j < sink_tokens).  window_tokens at
+ * least 1, sink_tokens at least 0; the plan's own sink_tokens, window_tokens, alpha and use_correction play no part.  Only blocks
+ * that some query of a tile sees are visited.  For layers with a sliding window: prompts and chunks of prompts; fp2_decode has
+ * the same mask for single tokens.
+ * Entries of pages that no query sees -- wholly in front of all windows and behind the sinks -- may be anything (pages that were
+ * given back).  What stands in places that no query of a 128-row tile sees, rows of a last page behind the sequence's end among
+ * them, never matters; V of a token that some query of a tile sees must be finite for the others.  Arguments and results otherwise
+ * as fp2_dense_prefill.  Two kernels on `stream`. */
+fp2_status fp2_window_prefill(fp2_plan* plan, const void* q, const void* k_cache, const void* v_cache,
+                              const int32_t* page_table, const int32_t* cu_seqlens_q, const int32_t* seqlens_k,
+                              const float* q_scale, const float* k_scale, const float* v_scale, int32_t window_tokens,
+                              int32_t sink_tokens, void* out, float* lse, void* workspace, fp2_stream stream);
+
 /* (No counterpart in the paper.)  fp2_dense_prefill for callers that have no device workspace to hand in and
  * may not create one: a plug-in whose host passes it fixed input and output buffers and forbids device
  * allocation, or code on a path where the memory allocator must not be entered (a framework callback, a

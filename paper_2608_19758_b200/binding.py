@@ -22,7 +22,7 @@ EXPORTS = ["fp2_plan_create", "fp2_plan_sizes", "fp2_plan_destroy", "fp2_plan_se
            "fp2_sparse_prefill", "fp2_dense_prefill", "fp2_dense_prefill_static", "fp2_export_csr",
            "fp2_page_table_from_token_map", "fp2_plan_set_split", "fp2_pool_carry", "fp2_pool_carry_count",
            "fp2_read_status", "fp2_selftest_bounded_wait", "fp2_last_launch_count", "fp2_status_string",
-           "fp2_cache_create", "fp2_cache_destroy", "fp2_cache_sizes", "fp2_cache_append", "fp2_cache_expand", "fp2_decode",
+           "fp2_window_prefill", "fp2_cache_create", "fp2_cache_destroy", "fp2_cache_sizes", "fp2_cache_append", "fp2_cache_expand", "fp2_decode",
            "fp2_cache_read_status"]
 
 
@@ -88,6 +88,9 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.fp2_dense_prefill_static.argtypes = [C.c_void_p, vp, vp, vp, i32p, i32p, i32p, f32p, f32p, f32p, vp, f32p,
                                              C.c_void_p]
     lib.fp2_dense_prefill_static.restype = C.c_int
+    lib.fp2_window_prefill.argtypes = [C.c_void_p, vp, vp, vp, i32p, i32p, i32p, f32p, f32p, f32p, C.c_int32, C.c_int32, vp, f32p,
+                                       vp, C.c_void_p]
+    lib.fp2_window_prefill.restype = C.c_int
     lib.fp2_export_csr.argtypes = [C.c_void_p, i32p, i32p, C.c_int32, i32p, i32p, C.c_int64, vp, C.c_void_p]
     lib.fp2_export_csr.restype = C.c_int
     lib.fp2_page_table_from_token_map.argtypes = [C.c_void_p, i32p, C.c_int32, i32p, i32p, vp, C.c_void_p]
@@ -241,6 +244,15 @@ def fp2_dense_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q,
                                     _ptr(cu_seqlens_q), _ptr(seqlens_k), _ptr(q_scale), _ptr(k_scale),
                                     _ptr(v_scale), _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)),
            "fp2_dense_prefill")
+
+
+def fp2_window_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale, v_scale,
+                       window_tokens: int, sink_tokens: int, out, lse, workspace, stream=None):
+    """Causal attention with a sliding window of `window_tokens` and the first `sink_tokens` tokens always visible."""
+    _check(load().fp2_window_prefill(plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+                                     _ptr(cu_seqlens_q), _ptr(seqlens_k), _ptr(q_scale), _ptr(k_scale), _ptr(v_scale),
+                                     window_tokens, sink_tokens, _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)),
+           "fp2_window_prefill")
 
 
 def fp2_dense_prefill_static(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale,

@@ -416,6 +416,13 @@ static auto pair_kernel(const DevParams& d) -> decltype(&score_pair_kernel<false
   return score_pair_kernel<true, 0>;
 }
 
+// The kernel of fp2_window_prefill; widen: see use_v16.
+static auto window_kernel(const fp2_plan* pl, bool widen) -> decltype(&sparse_attn_kernel<false, false, true>) {
+  if (!pl->dev.fp8) return sparse_attn_kernel<false, false, true>;
+  return widen ? sparse_attn_kernel<true, true, true> : sparse_attn_kernel<true, false, true>;
+}
+static int attn_smem(const fp2_plan* pl) { return pl->dev.fp8 ? AttnCfg<true>::kSmemBytes : AttnCfg<false>::kSmemBytes; }
+
 static fp2_status set_attrs(fp2_plan* pl) {
   if (pl->attrs_set) return FP2_OK;
   if (cudaFuncSetAttribute(pair_kernel(pl->dev), cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmemBytes) != cudaSuccess ||
@@ -423,22 +430,28 @@ static fp2_status set_attrs(fp2_plan* pl) {
                            kScoreSmemBytes) != cudaSuccess ||
       cudaFuncSetAttribute(score_select_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            kScoreSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(sparse_attn_kernel<false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      cudaFuncSetAttribute(sparse_attn_kernel<false, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            AttnCfg<false>::kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(sparse_attn_kernel<true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+      cudaFuncSetAttribute(sparse_attn_kernel<true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            AttnCfg<true>::kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(sparse_attn_kernel<true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           AttnCfg<true>::kSmemBytes) != cudaSuccess)
+      cudaFuncSetAttribute(sparse_attn_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           AttnCfg<true>::kSmemBytes) != cudaSuccess ||
+      cudaFuncSetAttribute(window_kernel(pl, true), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(pl)) != cudaSuccess ||
+      cudaFuncSetAttribute(window_kernel(pl, false), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(pl)) != cudaSuccess)
     return FP2_ERR_CUDA;
   // The attention kernels move registers between warps with setmaxnreg, whose wait is unbounded: launch only
   // if the compiled kernels really own the registers the move assumes.
   cudaFuncAttributes fa;
-  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<false, false>) != cudaSuccess) return FP2_ERR_CUDA;
+  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<false, false, false>) != cudaSuccess) return FP2_ERR_CUDA;
   if (fa.numRegs * AttnCfg<false>::kThreads < AttnCfg<false>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
-  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<true, false>) != cudaSuccess) return FP2_ERR_CUDA;
+  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<true, false, false>) != cudaSuccess) return FP2_ERR_CUDA;
   if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
-  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<true, true>) != cudaSuccess) return FP2_ERR_CUDA;
+  if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<true, true, false>) != cudaSuccess) return FP2_ERR_CUDA;
   if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
+  for (int widen = 0; widen < 2; ++widen) {
+    if (cudaFuncGetAttributes(&fa, window_kernel(pl, widen != 0)) != cudaSuccess) return FP2_ERR_CUDA;
+    if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
+  }
   pl->attrs_set = true;
   return FP2_OK;
 }
@@ -582,7 +595,8 @@ static void launch_attn(fp2_plan* pl, const CUtensorMap& mk, const CUtensorMap& 
                         int64_t max_units, bool widen, cudaStream_t st) {
   const int64_t workers = (int64_t)pl->num_sms * AttnCfg<false>::kCtasPerSm;
   const unsigned grid = (unsigned)(max_units < workers ? max_units : workers);
-  auto kernel = !pl->dev.fp8 ? sparse_attn_kernel<false, false> : widen ? sparse_attn_kernel<true, true> : sparse_attn_kernel<true, false>;
+  auto kernel = !pl->dev.fp8 ? sparse_attn_kernel<false, false, false>
+                : widen ? sparse_attn_kernel<true, true, false> : sparse_attn_kernel<true, false, false>;
   launch(kernel, grid, AttnCfg<false>::kThreads, pl->dev.fp8 ? AttnCfg<true>::kSmemBytes : AttnCfg<false>::kSmemBytes, st, mk,
          mv, mkb, mkb_lo, mvb, mq, a, pl->dev);
 }
@@ -704,6 +718,58 @@ extern "C" fp2_status fp2_dense_prefill(fp2_plan* pl, const void* q, const void*
                                         const int32_t* cu, const int32_t* lk, const float* qs, const float* ks,
                                         const float* vs, void* out, float* lse, void* workspace, fp2_stream stream) {
   return run_attention(pl, q, k, v, pt, cu, lk, nullptr, nullptr, qs, ks, vs, out, lse, workspace, false, stream);
+}
+
+// Sliding window and sinks: two launches, the second the attention kernel's LOCAL form.
+extern "C" fp2_status fp2_window_prefill(fp2_plan* pl, const void* q, const void* k, const void* v, const int32_t* pt,
+                                         const int32_t* cu, const int32_t* lk, const float* qs, const float* ks, const float* vs,
+                                         int32_t window_tokens, int32_t sink_tokens, void* out, float* lse, void* workspace,
+                                         fp2_stream stream) {
+  if (window_tokens < 1 || sink_tokens < 0 || !out_ok(pl, out)) return FP2_ERR_INVALID_ARG;
+  fp2_status s = check_common(pl, q, k, v, pt, cu, lk, qs, ks, vs, workspace);
+  if (s != FP2_OK) return s;
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
+  pl->last_launches = 0;
+  if (pl->nseg == 0) return FP2_OK;
+  const int most = kMaxBlocks * kBlock;   // (no position is further away; the kernel's sums stay in 32 bits)
+  const int window = std::min(window_tokens, most), sinks = std::min(sink_tokens, most);
+  // iterations of a segment: the blocks of the first row's window and of the rows behind it, and of the sinks
+  const int64_t per_seg = (int64_t)(window + kTileRows - 2) / kBlock + 2 + (sinks + kBlock - 1) / kBlock;
+  const bool use_v16 = pl->dev.fp8 && std::min(pl->idx_capacity, pl->nseg * per_seg) >= pl->v16_iters;
+  int32_t* const counter = reinterpret_cast<int32_t*>(ws + pl->ws_counter);
+  // Clears the work counter; FP8: V as F16.  What it finds of missing pages is not reported (words of the counter block that
+  // nothing reads): the attention kernel reports those that a query sees.
+  launch_at(!use_v16, attn_prepare_kernel, 1 + (use_v16 ? (unsigned)(pl->nblk_tot * (kBlock / kWidenTokens)) : 0u), 256, 0, st,
+            reinterpret_cast<int32_t*>(ws + pl->ws_hist), 0, counter, 1, (const uint8_t*)v, pt, pl->d_lk, pl->d_blk_off, pl->dev,
+            use_v16 ? reinterpret_cast<__half*>(ws + pl->ws_v16) : nullptr, counter + 8);
+  pl->last_launches += 1;
+  if (cudaGetLastError() != cudaSuccess) return FP2_ERR_CUDA;
+  const int64_t slots = (int64_t)pl->prm.num_pages * pl->prm.page_size;
+  CUtensorMap mk, mv, mq;
+  if (!make_map(pl, &mk, k, slots, pl->prm.num_kv_heads, pl->prm.page_size, pl->dev.fp8) ||
+      !(use_v16 ? make_map(pl, &mv, ws + pl->ws_v16, pl->nblk_tot * kBlock, pl->prm.num_kv_heads, kBlock, false)
+                : make_map(pl, &mv, v, slots, pl->prm.num_kv_heads, pl->prm.page_size, pl->dev.fp8)))
+    return FP2_ERR_CUDA;
+  mq = mk;   // unused unless q_box
+  if (pl->dev.q_box && !make_q_map(pl, &mq, q, pl->dev.q_box_tok)) return FP2_ERR_CUDA;
+  AttnArgs a = {};
+  a.q = reinterpret_cast<const uint8_t*>(q);
+  a.page_table = pt;
+  a.segs = pl->d_segs;
+  a.q_scale = qs; a.k_scale = ks; a.v_scale = vs;
+  a.out = reinterpret_cast<__nv_bfloat16*>(out);
+  a.lse = lse;
+  a.work_counter = counter;
+  a.status = reinterpret_cast<int*>(ws + pl->ws_status);
+  a.window = window;
+  a.sinks = sinks;
+  const int64_t workers = (int64_t)pl->num_sms * AttnCfg<false>::kCtasPerSm;
+  // (no pooled chunks: those maps are never dereferenced)
+  launch(window_kernel(pl, !use_v16), (unsigned)std::min(pl->nseg, workers), AttnCfg<false>::kThreads, attn_smem(pl), st, mk, mv, mk,
+         mk, mv, mq, a, pl->dev);
+  pl->last_launches += 1;
+  return cudaGetLastError() == cudaSuccess ? FP2_OK : FP2_ERR_CUDA;
 }
 
 // ------------------------------------------------------------------------------------------------------

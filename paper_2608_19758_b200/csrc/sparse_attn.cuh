@@ -62,6 +62,8 @@ struct TileInfo {
   int32_t it_begin, it_end;   // this unit's part of the iteration sequence [0, T + nchunk) (Eq. 18); all of it unless split
   int32_t parts;              // parts the segment is split into (1: the unit writes the final output)
   int32_t slot;               // partial-result slot of this unit when parts > 1
+  int32_t n_win;              // LOCAL: iterations of the window; those of the sinks follow
+  int32_t lo_tok, hi_tok;     // LOCAL: first token of the first row's window, position of the last row
   int32_t chunk_id[kMaxChunks];
   uint32_t todo[kMaxChunks][4];
 };
@@ -87,6 +89,7 @@ struct AttnArgs {
   const int32_t* n_units;
   float* part_o;
   float2* part_ml;
+  int32_t window, sinks;      // LOCAL: a query at position p sees the tokens j <= p with p - j < window or j < sinks
 #ifdef FP2_PROFILE
   long long* prof;   // [grid][16] cycle counters of the softmax warpgroup (development builds only)
 #endif
@@ -218,9 +221,29 @@ __device__ __forceinline__ float row_exp(const uint32_t (&x)[128], uint32_t p_ad
   return a0 + a1;
 }
 
+// LOCAL: rows of a V tile that some query of the tile sees, in block-relative tokens: up to hi, from lo on or below `sink`.
+struct VRows {
+  int lo, hi, sink;
+  __device__ __forceinline__ bool seen(int r) const { return r <= hi && (r >= lo || r < sink); }
+};
+
+// Another row may hold anything, NaN included, which no probability of zero makes harmless: it is cleared.  128 threads, a row each.
+__device__ __forceinline__ void clear_hidden_rows(uint8_t* sV, const VRows& vr, int row) {
+  if (vr.seen(row)) return;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    *reinterpret_cast<uint4*>(sV + row * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(sV + 16384 + row * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+  }
+}
+
 // map_kbar / map_kbar_lo: pooled keys of the correction chunks -- BF16: one BF16 array (map_kbar_lo unused);
 // FP8: the e4m3 hi and lo arrays.  map_vbar: pooled values, 16-bit.  map_q: packed query tiles (DevParams::q_box).
-template <bool FP8, bool WIDEN>
+// LOCAL: sliding window and sinks (fp2_window_prefill).  The iteration sequence of a unit is the blocks of its rows' windows, J_hi
+// downwards, then the blocks of the sinks in front of them; blocks that some row does not see whole (the diagonal, where the
+// windows begin, the last sink) are masked in tensor memory: what hidden keys hold (NaN) would come through a mask that the tensor
+// core adds.  Segments differ little in length, so they run in their own order.
+template <bool FP8, bool WIDEN, bool LOCAL = false>
 __global__ void __launch_bounds__(AttnCfg<FP8>::kThreads, AttnCfg<FP8>::kCtasPerSm)
 sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                     const __grid_constant__ CUtensorMap map_kbar, const __grid_constant__ CUtensorMap map_kbar_lo,
@@ -362,10 +385,16 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         break;
       }
-      const int seg = A.order[w];
+      const int seg = LOCAL ? w : A.order[w];
       const SegInfo sg = A.segs[seg];
-      const bool dense = A.seg_count == nullptr;
+      const bool dense = LOCAL || A.seg_count == nullptr;
       int T = dense ? sg.J_hi + 1 : A.seg_count[seg];
+      int lo_tok = 0, n_win = 0;
+      if constexpr (LOCAL) {
+        lo_tok = max(0, sg.pre + sg.r0 / g - A.window + 1);
+        n_win = sg.J_hi - lo_tok / kBlock + 1;
+        T = n_win + min((A.sinks + kBlock - 1) / kBlock, lo_tok / kBlock);
+      }
       if (T < 0 || T > sg.J_hi + 1) {  // malformed count: clamp so every loop stays bounded
         if (t64 == 0) atomicOr(A.status + ST_BAD_LIST, 1);
         T = max(0, min(T, sg.J_hi + 1));
@@ -420,7 +449,12 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           ti.dense = dense;
           ti.T = T;
           ti.nchunk = nchunk;
-          ti.ndiag = dense ? min(T, sg.J_hi - sg.J_lo + 1) : ndiag_s;
+          ti.ndiag = LOCAL ? 0 : dense ? min(T, sg.J_hi - sg.J_lo + 1) : ndiag_s;
+          if constexpr (LOCAL) {
+            ti.n_win = n_win;
+            ti.lo_tok = lo_tok;
+            ti.hi_tok = sg.pre + (sg.r0 + sg.nrows - 1) / g;
+          }
           ndiag_s = 0;
           ti.parts = parts;
           ti.slot = ((split >> 16) & 0xffff) + u;
@@ -486,11 +520,15 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       int J_fetched = 0;   // block id of the iteration fetch_pid was last asked for (warp-uniform)
       auto fetch_pid = [&](int i) -> int {
         if (i >= T) return -1;
-        int J = ti.dense ? sg.J_hi - i : list[T - 1 - i];
+        int J = LOCAL ? (i < ti.n_win ? sg.J_hi - i : T - 1 - i) : ti.dense ? sg.J_hi - i : list[T - 1 - i];
         J = max(0, min(J, sg.J_hi));
         J_fetched = J;
         if (lane >= ppb) return -1;
         if (J * kBlock + lane * psz >= sg.Lk) return -1;
+        if constexpr (LOCAL) {   // pages that no row of the tile sees are not looked at: they may be gone
+          const int t0 = J * kBlock + lane * psz;
+          if (t0 > ti.hi_tok || (t0 + psz <= ti.lo_tok && t0 >= A.sinks)) return -1;
+        }
         int pid = pt[J * ppb + lane];
         if (pid < 0 || pid >= P.num_pages) {
           atomicOr(A.status + ST_BAD_LIST, 2);
@@ -768,13 +806,30 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         bool need_mask = false;
         int tok_lim = 1 << 30;     // exact block: columns j with j <= tok_lim are visible
         uint32_t cm0 = 0xffffffffu, cm1 = 0xffffffffu, cm2 = 0xffffffffu, cm3 = 0xffffffffu;
+        VRows vr{0, kBlock, 0};   // LOCAL
+        (void)vr;
         float shift = 0.f;
         if (i < T) {
-          int J = dense ? J_hi - i : J_next;
+          int J = LOCAL ? (i < ti.n_win ? J_hi - i : T - 1 - i) : dense ? J_hi - i : J_next;
           if (!dense && i + 1 < T) J_next = list[T - 2 - i];
           J = max(0, min(J, J_hi));
           need_mask = J >= J_lo && (!P.diag_mma || weak_bias);   // else the causal mask is in the logits already
           tok_lim = pos - J * kBlock;
+          if constexpr (LOCAL) {
+            const int t0 = J * kBlock;
+            vr = {ti.lo_tok - t0, ti.hi_tok - t0, A.sinks - t0};
+            need_mask = J >= J_lo || (t0 <= ti.hi_tok - A.window && t0 + kBlock > A.sinks);
+            if (need_mask) {   // columns from pos - window + 1 on, and sinks
+              const int lo = tok_lim - A.window + 1;
+              auto bits = [&](int k) {
+                return __funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, lo - 32 * k))) | ~__funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, vr.sink - 32 * k)));
+              };
+              cm0 = bits(0);
+              cm1 = bits(1);
+              cm2 = bits(2);
+              cm3 = bits(3);
+            }
+          }
         } else {
           shift = 7.0f;  // log2(128): one pooled row stands for a full block (Eq. 6); the todo mask is in the logits already
           if (weak_bias) {
@@ -794,7 +849,16 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           if (i < T) {
             mbar_wait(&vraw_full, rc & 1, ctx, 603);
             if (G >= 1) wait_pv(G - 1, 602);
-            widen_tile_f16(sVraw, sV, tid, 128);
+            if constexpr (LOCAL) {
+#pragma unroll 4
+              for (int k = tid; k < kTileRows * 8; k += 128) {
+                uint4 v = *reinterpret_cast<const uint4*>(sVraw + sw128_offset(k >> 3, k & 7));
+                if (!vr.seen(k >> 3)) v = make_uint4(0, 0, 0, 0);
+                widen_chunk_f16(v, sV, k >> 3, k & 7);
+              }
+            } else {
+              widen_tile_f16(sVraw, sV, tid, 128);
+            }
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {   // (no barrier between the warps: after an abort one of them may have left)
@@ -812,6 +876,13 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #endif
         tc_fence_after();
         if (need_mask) mask_row(s_addr, tok_lim, cm0, cm1, cm2, cm3);
+        if constexpr (LOCAL && !WIDEN) {
+          if (need_mask && (vr.hi < kBlock - 1 || (vr.lo > 0 && vr.sink < vr.lo))) {
+            mbar_wait(&v_full, G & 1, ctx, 504);
+            clear_hidden_rows(sV, vr, row);
+            fence_proxy_async();   // (O += P V starts when all threads have arrived on the first slice of P)
+          }
+        }
         PF_END(4);
         uint32_t x[128];
         const float mx = fmaf(row_load_max(s_addr, x), cs_all, shift);  // cs > 0: scaling commutes with the maximum

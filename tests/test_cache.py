@@ -131,3 +131,20 @@ def test_binding_refuses_tensors_that_are_not_what_the_address_is_taken_for():
             binding.fp2_cache_expand(cache, **{**good, name: bad})
         assert e.value.code == 1, name
     cache.close()
+
+
+@pytest.mark.parametrize("window,sinks,code", [(0, 4, 1), (-1, 0, 1), (4, -1, 1), (1, 0, 4), (2 ** 31 - 1, 2 ** 31 - 1, 4)])
+def test_window_prefill_refuses(window, sinks, code):
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    prm = dict(num_seqs=1, total_q=300, num_q_heads=8, num_kv_heads=2, head_dim=128, block_size=128, tile_rows=128, page_size=16,
+               num_pages=64, max_pages_per_seq=32, sink_tokens=256, window_tokens=512, use_correction=1, alpha=0.1,
+               softmax_scale=0.0, dtype=1)
+    plan = binding.Plan(prm, [0, 300], [400])
+    lib, p = binding.load(), C.c_void_p(4096)
+    assert lib.fp2_window_prefill(plan.handle, p, p, p, p, p, p, p, p, p, window, sinks, p, None, p, None) == code
+    for bad in (dict(q=None), dict(q=4104), dict(out=4112), dict(out=None), dict(ws=512), dict(qs=None), dict(pt=None)):
+        a = dict(dict(q=4096, pt=4096, qs=4096, out=4096, ws=4096), **bad)
+        assert lib.fp2_window_prefill(plan.handle, a["q"], p, p, a["pt"], p, p, a["qs"], p, p, 16, 0, a["out"], None, a["ws"], None) == 1
+    assert lib.fp2_window_prefill(None, p, p, p, p, p, p, p, p, p, 16, 0, p, None, p, None) == 1
+    plan.close()
