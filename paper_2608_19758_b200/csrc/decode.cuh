@@ -5,26 +5,28 @@
 //
 // Bound by the bytes of the cache: each is wanted once, the arithmetic of a group of query heads on them is small.  So:
 //
-// Work split.  The (sequence, KV head, tile of packed rows, 64-token block) items are numbered in that order, and every CTA of a
+// Work split.  The (sequence, KV head, tile of packed rows, block of tokens) items are numbered in that order, and every CTA of a
 // grid that fills the GPU takes an equal contiguous share, whatever the lengths: a long sequence is cut wherever shares end.  The
 // lengths are read on the device (a captured graph stays valid as sequences grow), so the CTAs find their shares themselves.  A
 // unit (sequence, head, tile) cut into parts leaves (O, m, l) of each in the workspace, and the CTA that arrives last joins them,
 // in the order of the shares: the result does not depend on who is last.  One launch.
 //
-// A CTA is four warps, two CTAs to an SM.  Of a block each warp takes 16 tokens, which it copies into its own part of shared
-// memory (cp.async, kStages steps ahead) and attends to with its own running maximum and sum: no barrier in the loop; the
-// four join at the end of a unit.  Copies of hidden tokens write zeros without reading, so nothing that stands in a hidden place
-// reaches the sums.  192 KB in flight per SM.
+// A CTA is four warps, two CTAs to an SM.  Of a block each warp takes a step of kTok tokens (8 KB), which it copies into its own
+// part of shared memory (cp.async, kStages steps ahead) and attends to with its own running maximum and sum: no barrier in the
+// loop; the four join at the end of a unit, while the first copies of the next one are on their way.  Copies of hidden tokens
+// write zeros without reading, so nothing that stands in a hidden place reaches the sums.  192 KB of an SM take part.
 //
-// S = Q K^T and O += P V are m16n8k16 MMAs of a warp, rows = 16 packed (token, query head) pairs of the KV head, MT of these: what
-// tcgen05 would add in rate is not what bounds this, and its 64 rows and round trips through tensor memory are what a group of
-// eight heads has no use for.  K and V are read from shared memory 16 bytes a lane; which of a lane's values play which index of
-// the contraction (over dims in Q K^T) or which column (dims in P V) is free, as long as Q is permuted alike and O stored
-// accordingly, so that no transposing is needed but pairing two tokens' values by byte permutation.
+// S^T = K Q^T and O^T += V^T P^T are m16n8k16 MMAs of a warp with the tokens (then the dims) as the long side and 8 packed
+// (token, query head) rows of the KV head as the short one, NR times: a group of up to eight heads wastes nothing.  What tcgen05
+// would add in rate is not what bounds this, and its 64 rows are what such a group has no use for.  K and V are read from shared
+// memory 16 bytes a lane; which of a lane's values play which index of the contraction over dims in K Q^T, or which row (a dim) of
+// V^T, is free as long as Q is permuted alike and O stored accordingly, so nothing is transposed but P (8 x 8 at a time, one
+// instruction) and pairs of tokens of V (byte permutation).
 //
 // Precision.  BF16 caches: Q and K as they are; P as a BF16 pair hi + lo (2^-17).  e4m3 caches: K, V exact as F16; Q exact as
 // F16 after a power of two per row has brought its maximum to 2^13 .. 2^14 (elements 2^-28 below it round); P as F16 against a
 // reference 8 binades below the running maximum, where the steps are 2^-11 relative down to 2^-22 of the maximum.  Sums in 32 bits.
+// (e4m3 operands as such: the warp-level MMA takes them, but widens them itself on this GPU, in more instructions than here.)
 // Scales per page: ks multiplies the logits; vs enters P, in the exponent, so that P V needs none:
 // y = x + log2 vs has the running maximum, p = 2^(y - m), and l adds p / vs.
 #pragma once
@@ -38,17 +40,25 @@ namespace fp2 {
 constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kDecCtasPerSm = 2;
-constexpr int kDecBlock = 16 * kDecWarps;     // tokens of a work item
-constexpr int kDecMinShare = 2;               // blocks per CTA below which more CTAs do not pay
+constexpr int kDecMinShare = 4;               // least share of a CTA, in blocks (kDecUnitCost included)
+constexpr int kDecUnitCost = 2;               // what a unit costs beside its blocks, in blocks
 
-template <int FMT>
+template <int FMT, int NR>
 struct DecodeCfg {
-  static constexpr int kEsz = FMT == FMT_BF16 ? 2 : 1;
-  static constexpr int kHalf = 16 * 128;                          // 16 rows of 128 bytes
-  static constexpr int kTile = kHalf * kEsz;                      // K (or V) of 16 tokens of a head
-  static constexpr int kStages = FMT == FMT_BF16 ? 3 : 6;
-  static constexpr int kRing = kDecWarps * kStages * 2 * kTile;   // 96 KB
-  static constexpr int kSmemBytes = 128 + kRing;
+  static constexpr bool kFp8 = FMT != FMT_BF16;
+  static constexpr int kEsz = kFp8 ? 1 : 2;
+  static constexpr int kTok = kFp8 ? 32 : 16;                     // tokens of a step
+  static constexpr int kBlock = kTok * kDecWarps;                 // tokens of a work item
+  static constexpr int kHalf = kTok * 128;                        // kTok rows of 128 bytes
+  static constexpr int kTile = kHalf * kEsz;                      // K (or V) of a step, of one head: 4 KB
+  static constexpr int kStep = 2 * kTile;
+  static constexpr int kStages = 3;
+  static constexpr int kRing = kStages * kStep;                   // of a warp
+  static constexpr int kRows = 8 * NR;
+  // stages that may be filled for the next unit while the warps' results of this one are joined in the others
+  static constexpr int kEarly = (kRing - kRows * kHeadDim * 4) / kStep;
+  static_assert(kEarly >= 1 && kEarly < kStages, "the join needs room, the next unit a start");
+  static constexpr int kSmemBytes = 128 + kDecWarps * kRing;      // 96 KB
 };
 
 struct DecodeArgs {
@@ -59,8 +69,8 @@ struct DecodeArgs {
   const float *k_scale, *v_scale;
   __nv_bfloat16* out;
   float* lse;
-  float* part_o;                // [2 grid][16 MT][128]
-  float2* part_ml;              // [2 grid][16 MT]
+  float* part_o;                // [2 grid][8 NR][128]
+  float2* part_ml;              // [2 grid][8 NR]
   int32_t* counters;            // [grid], zero between calls
   int* status;
   int32_t total_q, num_q_heads, group, window, sinks;
@@ -73,11 +83,12 @@ struct DecodeSeq {
   int c0, Lq, L;      // first query row, queries, tokens in the cache
   int ntiles;         // tiles of packed rows of a KV head
   int sb, wb0, nblk;  // blocks: 0 .. sb - 1 (sinks), then wb0 .. ; nblk in all
-  long long cost;     // items
+  long long cost;     // blocks of all units, kDecUnitCost more for each
 };
 
-template <int RT>
+template <typename Cfg>
 __device__ __forceinline__ DecodeSeq decode_seq(const DecodeArgs& A, int b, bool report) {
+  constexpr int B = Cfg::kBlock;
   DecodeSeq s;
   s.c0 = A.cu[b];
   const int c1 = A.cu[b + 1];
@@ -89,29 +100,46 @@ __device__ __forceinline__ DecodeSeq decode_seq(const DecodeArgs& A, int b, bool
     s.L = 0;
     s.c0 = 0;
   }
-  s.ntiles = (int)(((long long)A.group * s.Lq + RT - 1) / RT);
+  s.ntiles = (int)(((long long)A.group * s.Lq + Cfg::kRows - 1) / Cfg::kRows);
   // tokens some query sees: below the sinks, and from the first query's window on
   const int first = s.L - s.Lq;
   const int lo = A.window > 0 ? max(0, (int)min((long long)s.L, (long long)first - A.window + 1)) : 0;
-  s.wb0 = lo / kDecBlock;
-  s.sb = min((int)(((long long)min(A.sinks, s.L) + kDecBlock - 1) / kDecBlock), s.wb0);
-  s.nblk = max(1, s.sb + (s.L + kDecBlock - 1) / kDecBlock - s.wb0);   // (one for rows that see nothing: they are written)
-  s.cost = (long long)s.ntiles * A.g.num_kv_heads * s.nblk;
+  s.wb0 = lo / B;
+  s.sb = min((int)(((long long)min(A.sinks, s.L) + B - 1) / B), s.wb0);
+  s.nblk = max(1, s.sb + (s.L + B - 1) / B - s.wb0);   // (one for rows that see nothing: they are written)
+  s.cost = (long long)s.ntiles * A.g.num_kv_heads * (s.nblk + kDecUnitCost);
   return s;
 }
 
-__device__ __forceinline__ void mma_16816_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16816_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_16816_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_16816_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void cp_async4(uint32_t smem_dst, const void* gsrc, uint32_t src_bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_dst), "l"(gsrc), "r"(src_bytes) : "memory");
+// 8 x 8 matrix of 16-bit elements, row i in the lanes 4 i .. 4 i + 3: transposed
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+// four e4m3 bytes -> two pairs of F16 (exact)
+__device__ __forceinline__ void e4m3x4_to_f16x4(uint32_t x, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 l, h;\n mov.b32 {l, h}, %2;\n cvt.rn.f16x2.e4m3x2 %0, l;\n cvt.rn.f16x2.e4m3x2 %1, h;\n}" : "=r"(lo), "=r"(hi) : "r"(x));
+}
+// 16 bytes global -> shared; zeros without reading
+__device__ __forceinline__ void cp_async16(uint32_t smem_dst, const void* gsrc) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_dst), "l"(gsrc) : "memory");
+}
+__device__ __forceinline__ void cp_async16_if(uint32_t smem_dst, const void* gsrc, bool read) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_dst), "l"(gsrc), "r"(read ? 16u : 0u) : "memory");
+}
+__device__ __forceinline__ void cp_async4_if(uint32_t smem_dst, const void* gsrc, bool read) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_dst), "l"(gsrc), "r"(read ? 4u : 0u) : "memory");
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
   uint4 r;
@@ -119,15 +147,27 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   return r;
 }
 
-template <int FMT, int MT>
+// A unit's part of this CTA: blocks i0 .. i1 - 1 of it
+struct DecodeUnit {
+  int b, h, r0, nrows;
+  int c0, first_pos, L, sb, wb0;
+  int pmin, pmax;              // positions of the first and last row
+  int i0, i1;
+  bool whole;
+  int w0, parts;               // CTAs that share the unit: the first one, how many
+};
+
+template <int FMT, int NR>
 __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm)
 decode_kernel(DecodeArgs A) {
-  using Cfg = DecodeCfg<FMT>;
-  constexpr bool FP8 = FMT != FMT_BF16;
-  constexpr int RT = 16 * MT, ST = Cfg::kStages;
+  using Cfg = DecodeCfg<FMT, NR>;
+  constexpr bool FP8 = Cfg::kFp8;
+  constexpr int RT = Cfg::kRows, ST = Cfg::kStages, TOK = Cfg::kTok;
+  constexpr int G = TOK / 8;             // groups of eight tokens of a step: what a page holds at least
+  constexpr uint32_t kAllLive = TOK == 32 ? 0xffffffffu : (1u << TOK) - 1u;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
-  __shared__ float page_scales[kDecWarps][ST][4];          // PAGE: ks of tokens 0..7, 8..15, then vs
+  __shared__ float page_scales[kDecWarps][ST][2 * G];      // PAGE: ks of the groups, then vs
   __shared__ uint32_t live_s[kDecWarps][ST];               // tokens of the step that were copied
   __shared__ float2 ml_s[kDecWarps][RT];
   __shared__ long long scan_s[kDecWarps];
@@ -143,7 +183,7 @@ decode_kernel(DecodeArgs A) {
   // ------------------------------ this CTA's share ------------------------------
   long long total = 0;
   for (int b0 = 0; b0 < A.g.num_seqs; b0 += kDecThreads)
-    total += b0 + tid < A.g.num_seqs ? decode_seq<RT>(A, b0 + tid, blockIdx.x == 0).cost : 0;
+    total += b0 + tid < A.g.num_seqs ? decode_seq<Cfg>(A, b0 + tid, blockIdx.x == 0).cost : 0;
 #pragma unroll
   for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   if (lane == 0) scan_s[warp] = total;
@@ -159,7 +199,7 @@ decode_kernel(DecodeArgs A) {
   {
     long long base = 0;
     for (int b0 = 0; b0 < A.g.num_seqs; b0 += kDecThreads) {
-      const long long cost = b0 + tid < A.g.num_seqs ? decode_seq<RT>(A, b0 + tid, false).cost : 0;
+      const long long cost = b0 + tid < A.g.num_seqs ? decode_seq<Cfg>(A, b0 + tid, false).cost : 0;
       long long incl = cost;
 #pragma unroll
       for (int d = 1; d < 32; d <<= 1) {
@@ -187,389 +227,489 @@ decode_kernel(DecodeArgs A) {
   }
   int b = found_b;
   long long seq_base = found_base;
-  DecodeSeq sq = decode_seq<RT>(A, b, false);
-
-  const uint32_t ring = smem_u32(smem) + warp * (ST * 2 * Cfg::kTile);
-  const uint32_t my_scales = smem_u32(&page_scales[warp][0][0]);
-  const uint64_t stream_pol = l2_policy_evict_first();
-
-  while (pos < pos_end) {
-    while (pos >= seq_base + sq.cost) {
-      seq_base += sq.cost;
-      sq = decode_seq<RT>(A, ++b, false);
+  DecodeSeq sq = decode_seq<Cfg>(A, b, false);
+  // Next unit of the share.  A unit takes kDecUnitCost places in front of its blocks' in the numbering.
+  auto next_unit = [&](DecodeUnit& u) -> bool {
+    while (pos < pos_end) {
+      while (pos >= seq_base + sq.cost) {
+        seq_base += sq.cost;
+        sq = decode_seq<Cfg>(A, ++b, false);
+      }
+      const int ulen = sq.nblk + kDecUnitCost;
+      const long long unit = (pos - seq_base) / ulen;
+      const long long unit0 = seq_base + unit * ulen;
+      u.i0 = max(0, (int)(pos - unit0) - kDecUnitCost);
+      u.i1 = max(0, (int)min((long long)ulen, pos_end - unit0) - kDecUnitCost);
+      pos = min(unit0 + ulen, pos_end);
+      if (u.i0 >= u.i1) continue;
+      u.b = b;
+      u.h = (int)(unit / sq.ntiles);
+      u.r0 = (int)(unit % sq.ntiles) * RT;
+      u.nrows = min(RT, grp * sq.Lq - u.r0);
+      u.c0 = sq.c0;
+      u.first_pos = sq.L - sq.Lq;
+      u.L = sq.L;
+      u.sb = sq.sb;
+      u.wb0 = sq.wb0;
+      u.pmin = u.first_pos + u.r0 / grp;
+      u.pmax = u.first_pos + (u.r0 + u.nrows - 1) / grp;
+      u.whole = u.i0 == 0 && u.i1 == sq.nblk;
+      u.w0 = (int)((unit0 + kDecUnitCost) / share);
+      u.parts = (int)((unit0 + ulen - 1) / share) - u.w0 + 1;
+      return true;
     }
-    const long long unit = (pos - seq_base) / sq.nblk;
-    const long long unit0 = seq_base + unit * sq.nblk;
-    const int i0 = (int)(pos - unit0), i1 = (int)min((long long)sq.nblk, pos_end - unit0);
-    const int h = (int)(unit / sq.ntiles), t = (int)(unit % sq.ntiles);
-    const int r0 = t * RT;
-    const int nrows = min(RT, grp * sq.Lq - r0);
-    const int first_pos = sq.L - sq.Lq;
-    const int pmin = first_pos + r0 / grp, pmax = first_pos + (r0 + nrows - 1) / grp;
-    const int32_t* pt = A.page_table + (size_t)b * A.g.max_pages;
+    return false;
+  };
+
+  // ------------------------------ copies ------------------------------
+  const uint32_t ring = smem_u32(smem) + warp * Cfg::kRing;
+  constexpr int kLanes = 8 * Cfg::kEsz;                    // lanes per row, 16 bytes each
+  constexpr int kRowsPer = 32 / kLanes;                    // rows per instruction
+  constexpr int kPerGroup = 8 / kRowsPer;                  // instructions per group of eight rows
+  const uint32_t row_bytes = (uint32_t)heads * (kHeadDim * Cfg::kEsz);
+  const int ch = lane % kLanes, rsub = lane / kLanes;
+  const uint32_t dst_lane = ring + (ch >> 3) * Cfg::kHalf + rsub * 128 + (((ch & 7) ^ rsub) << 4);
+  auto token0 = [&](const DecodeUnit& u, int i) { return Cfg::kBlock * (i < u.sb ? i : u.wb0 + i - u.sb) + warp * TOK; };
+  // Page ids of 32 / G steps: lane G k + j holds the one of step k's tokens 8 j .. 8 j + 7
+  auto load_pids = [&](const DecodeUnit& u, int i) -> int {
+    i += lane / G;
+    const int tok = token0(u, i) + (lane % G) * 8;
+    return i < u.i1 && tok < u.L ? A.page_table[(size_t)u.b * A.g.max_pages + (tok >> shift)] : -1;
+  };
+  int pids = -1, pids_next = -1;
+  auto issue = [&](const DecodeUnit& u, int k, int slot) {           // step k of the unit's part, into stage `slot`
+    const int i = u.i0 + k;
+    if (i < u.i1) {
+      const int k0 = k % (32 / G) * G;
+      if (k0 == 0) {
+        pids = pids_next;
+        pids_next = load_pids(u, i + 32 / G);
+      }
+      const int t0 = token0(u, i);
+      int pid[G];
+      bool there = true;
+#pragma unroll
+      for (int j = 0; j < G; ++j) {
+        pid[j] = __shfl_sync(0xffffffffu, pids, k0 + j);
+        there &= (uint32_t)pid[j] < (uint32_t)A.g.num_pages;
+      }
+      const bool full = there && t0 + TOK - 1 <= u.pmax && (A.window <= 0 || t0 > u.pmin - A.window || t0 + TOK - 1 < A.sinks);
+      const uint32_t dst = dst_lane + slot * Cfg::kStep;
+      const uint32_t head_off = (uint32_t)u.h * (kHeadDim * Cfg::kEsz) + ch * 16;
+      const int mask = (1 << shift) - 1;
+      const uint8_t *kp = A.k + head_off, *vp = A.v + head_off;
+      uint32_t live = kAllLive;
+      if (full) {
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          const uint32_t row = ((uint32_t)pid[j] << shift) + ((t0 + 8 * j) & mask) + rsub;   // (slots of the pool: 31 bits)
+#pragma unroll
+          for (int q = 0; q < kPerGroup; ++q) {
+            const uint64_t off = (uint64_t)(row + q * kRowsPer) * row_bytes;
+            const uint32_t d = (dst ^ ((q * kRowsPer) << 4)) + (j * 8 + q * kRowsPer) * 128;
+            cp_async16(d, kp + off);
+            cp_async16(d + Cfg::kTile, vp + off);
+          }
+        }
+      } else {
+        const int my = (lane % TOK) / 8, tok = t0 + lane % TOK;
+        int p = pid[0];
+#pragma unroll
+        for (int j = 1; j < G; ++j) p = my == j ? pid[j] : p;
+        const bool wanted = tok <= u.pmax && tok < u.L && (A.window <= 0 || tok > u.pmin - A.window || tok < A.sinks);
+        const bool ok = (uint32_t)p < (uint32_t)A.g.num_pages;
+        if (__any_sync(0xffffffffu, wanted && !ok) && lane == 0) atomicOr(A.status + kCacheStBad, kBadPage);
+        live = __ballot_sync(0xffffffffu, wanted && ok) & kAllLive;
+        if (live != 0u) {
+#pragma unroll 1
+          for (int r = rsub; r < TOK; r += kRowsPer) {
+            const bool read = (live >> r) & 1u;
+            const int pr = __shfl_sync(0xffffffffu, p, r);           // (rows of one group in all lanes: its page)
+            const uint64_t off = read ? (uint64_t)(((uint32_t)pr << shift) + ((t0 + r) & mask)) * row_bytes : 0;
+            const uint32_t d = ring + slot * Cfg::kStep + (ch >> 3) * Cfg::kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+            cp_async16_if(d, kp + off, read);
+            cp_async16_if(d + Cfg::kTile, vp + off, read);
+          }
+        }
+      }
+      if (lane == 0) live_s[warp][slot] = live;
+      if constexpr (FMT == FMT_FP8_PAGE) {
+        if (lane < 2 * G) {
+          int p = pid[0];
+#pragma unroll
+          for (int j = 1; j < G; ++j) p = lane % G == j ? pid[j] : p;
+          const bool ok = ((live >> (lane % G * 8)) & 0xffu) != 0u;
+          cp_async4_if(smem_u32(&page_scales[warp][slot][lane]), (lane < G ? A.k_scale : A.v_scale) + (ok ? (size_t)p * heads + u.h : 0), ok);
+        }
+      }
+    }
+    cp_async_commit();
+  };
+
+  DecodeUnit u;
+  if (!next_unit(u)) return;
+  pids_next = load_pids(u, u.i0);
+#pragma unroll 1
+  for (int k = 0; k < Cfg::kEarly; ++k) issue(u, k, k);
+  for (;;) {
+#pragma unroll 1
+    for (int k = Cfg::kEarly; k < ST - 1; ++k) issue(u, k, k);
 
     // ------------------------------ queries ------------------------------
-    // Lane (l4, c) holds rows l4 and l4 + 8 of each 16-row tile; contraction step s covers, for it, the dims dim_of(s) .. + 3.
-    auto dim_of = [&](int s) { return FP8 ? 32 * c + 4 * s : 64 * (s >> 2) + 16 * c + 4 * (s & 3); };
-    uint32_t qa[MT][8][4];
-    float cs[MT][2];
-    int prow[MT][2];
+    // Lane (l4, c) holds row l4 of each 8-row tile, and of the contraction the dims that its 16-byte pieces of K hold: step s,
+    // dims 32 c + 4 s .. + 3 (e4m3) or 64 (s >> 2) + 16 c + 4 (s & 3) .. + 3 (BF16).
+    uint32_t qb[NR][8][2];
+    float cs[NR][2];                     // multipliers of rows 2 c, 2 c + 1: what a lane's logits belong to
+    int prow[NR][2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NR; ++n) {
+      const int r = u.r0 + min(n * 8 + l4, u.nrows - 1);
+      const int tok = r / grp, head = u.h * grp + r - tok * grp;
+      const uint8_t* src = A.q + (long long)(u.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2);
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int row = mt * 16 + u * 8 + l4;
-        const int r = r0 + min(row, nrows - 1);
-        const int tok = r / grp, head = h * grp + r - tok * grp;
-        prow[mt][u] = first_pos + tok;
-        const uint8_t* src = A.q + (long long)(sq.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2);
-        uint32_t w[16];
-#pragma unroll
-        for (int s = 0; s < 8; s += 2) {
-          const uint4 v = *reinterpret_cast<const uint4*>(src + dim_of(s) * 2);
-          w[2 * s] = v.x; w[2 * s + 1] = v.y; w[2 * s + 2] = v.z; w[2 * s + 3] = v.w;
-        }
-        cs[mt][u] = A.scale_log2;
-        if constexpr (FP8) {
-          uint32_t a = 0;
-#pragma unroll
-          for (int k = 0; k < 16; ++k) a = max(a, max(w[k] & 0x7fffu, (w[k] >> 16) & 0x7fffu));
-          a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
-          a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
-          // power of two that brings the row's maximum to [2^13, 2^14): 2^(13 + 127 - e)
-          int e = 140 - (int)(a >> 7);
-          e = a == 0 || a >= 0x7f80u ? 0 : max(-126, min(126, e));
-          const float f = __uint_as_float((uint32_t)(e + 127) << 23), back = __uint_as_float((uint32_t)(127 - e) << 23);
-          cs[mt][u] *= back;
-          if constexpr (FMT == FMT_FP8_HEAD) cs[mt][u] *= A.k_scale[h];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) w[k] = pack_f16x2(bf16_lo(w[k]) * f, bf16_hi(w[k]) * f);
-        }
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-          qa[mt][s][u] = w[2 * s];
-          qa[mt][s][u + 2] = w[2 * s + 1];
-        }
+      for (int s = 0; s < 8; s += 2) {
+        const uint4 x = *reinterpret_cast<const uint4*>(src + 2 * (FP8 ? 32 * c + 4 * s : 64 * (s >> 2) + 16 * c + 4 * (s & 3)));
+        qb[n][s][0] = x.x;
+        qb[n][s][1] = x.y;
+        qb[n][s + 1][0] = x.z;
+        qb[n][s + 1][1] = x.w;
       }
-
-    // ------------------------------ copies ------------------------------
-    auto token0 = [&](int i) { return kDecBlock * (i < sq.sb ? i : sq.wb0 + i - sq.sb) + warp * 16; };
-    // pages of the step's tokens 0..7 and 8..15 (the same one unless pages hold eight); -1: none.  Asked for one step ahead.
-    int pid0 = -1, pid1 = -1;
-    auto fetch_pages = [&](int i) {
-      pid0 = pid1 = -1;
-      if (i >= i1) return;
-      const int t0 = token0(i);
-      if (t0 < sq.L) pid0 = pt[t0 >> shift];
-      pid1 = shift >= 4 ? pid0 : t0 + 8 < sq.L ? pt[(t0 + 8) >> shift] : -1;
-    };
-    auto issue = [&](int i) {
-      if (i < i1) {
-        const int slot = (i - i0) % ST;
-        const int t0 = token0(i);
-        const int row = lane & 15, tok = t0 + row;
-        const int pid = row < 8 ? pid0 : pid1;
-        const bool wanted = tok <= pmax && tok < sq.L && (A.window <= 0 || tok > pmin - A.window || tok < A.sinks);
-        const bool there = pid >= 0 && pid < A.g.num_pages;
-        if (__any_sync(0xffffffffu, wanted && !there) && lane == 0) atomicOr(A.status + kCacheStBad, kBadPage);
-        const uint32_t live = __ballot_sync(0xffffffffu, wanted && there) & 0xffffu;
-        if (lane == 0) live_s[warp][slot] = live;
-        const uint32_t dst = ring + slot * 2 * Cfg::kTile;
-        if (live) {
-          const int page_row = t0 & ((1 << shift) - 1);
-          constexpr int kLanes = 8 * Cfg::kEsz;           // lanes per row, 16 bytes each
-          const int ch = lane % kLanes;
+      float mul = A.scale_log2;
+      if constexpr (FP8) {
+        uint32_t a = 0;
 #pragma unroll
-          for (int k = 0; k < 16 * kLanes / 32; ++k) {
-            const int r = k * (32 / kLanes) + lane / kLanes;
-            const uint32_t bytes = (live >> r) & 1u ? 16u : 0u;
-            const int p = r < 8 ? pid0 : pid1;
-            const int prow_ = shift >= 4 ? page_row + r : r & 7;
-            const size_t off = bytes ? ((((size_t)p << shift) + prow_) * heads + h) * (kHeadDim * Cfg::kEsz) + ch * 16 : 0;
-            const uint32_t d = dst + (ch >> 3) * Cfg::kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-            cp_async16(d, A.k + off, bytes, stream_pol);
-            cp_async16(d + Cfg::kTile, A.v + off, bytes, stream_pol);
-          }
-          if constexpr (FMT == FMT_FP8_PAGE) {
-            if (lane < 4) {
-              const int p = lane & 1 ? pid1 : pid0;
-              const bool ok = (live & (lane & 1 ? 0xff00u : 0xffu)) != 0u;
-              cp_async4(my_scales + (slot * 4 + lane) * 4, (lane < 2 ? A.k_scale : A.v_scale) + (ok ? (size_t)p * heads + h : 0),
-                        ok ? 4u : 0u);
-            }
-          }
-        }
-        fetch_pages(i + 1);
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) a = max(a, max(qb[n][s][k] & 0x7fffu, (qb[n][s][k] >> 16) & 0x7fffu));
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 1));
+        a = max(a, __shfl_xor_sync(0xffffffffu, a, 2));
+        // power of two that brings the row's maximum to [2^13, 2^14): 2^(13 + 127 - e)
+        int e = 140 - (int)(a >> 7);
+        e = a == 0 || a >= 0x7f80u ? 0 : max(-126, min(126, e));
+        const float f = __uint_as_float((uint32_t)(e + 127) << 23), back = __uint_as_float((uint32_t)(127 - e) << 23);
+        mul *= back;
+        if constexpr (FMT == FMT_FP8_HEAD) mul *= A.k_scale[u.h];
+        mul = fmaxf(mul, 1e-37f);        // (a hidden logit of -inf times zero would be NaN)
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+          for (int k = 0; k < 2; ++k) qb[n][s][k] = pack_f16x2(bf16_lo(qb[n][s][k]) * f, bf16_hi(qb[n][s][k]) * f);
       }
-      cp_async_commit();
-    };
-
-    float o[MT][16][4];
-    float m[MT][2], l[MT][2];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-      for (int j = 0; j < 16; ++j) o[mt][j][0] = o[mt][j][1] = o[mt][j][2] = o[mt][j][3] = 0.f;
-      m[mt][0] = m[mt][1] = -INFINITY;
-      l[mt][0] = l[mt][1] = 0.f;
+      for (int v = 0; v < 2; ++v) {      // from the lanes of row 2 c + v
+        cs[n][v] = __shfl_sync(0xffffffffu, mul, (2 * c + v) * 4);
+        prow[n][v] = u.first_pos + __shfl_sync(0xffffffffu, tok, (2 * c + v) * 4);
+      }
     }
-    fetch_pages(i0);
-#pragma unroll 1
-    for (int k = 0; k < ST - 1; ++k) issue(i0 + k);
+    DecodeUnit un;                       // the next one: known early, so that its page ids are there when this one ends
+    const bool more = next_unit(un);
+    const int pids_un = more ? load_pids(un, un.i0) : -1;
+
+    float o[NR][8][4];                   // tile t: rows 2 c, 2 c + 1 of two dims of this lane's
+    float m[NR][2], l[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+#pragma unroll
+      for (int t = 0; t < 8; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
+      m[n][0] = m[n][1] = -INFINITY;
+      l[n][0] = l[n][1] = 0.f;
+    }
 
     // ------------------------------ steps ------------------------------
+    int slot = 0, fill = ST - 1;
 #pragma unroll 1
-    for (int i = i0; i < i1; ++i) {
+    for (int i = u.i0; i < u.i1; ++i) {
       cp_async_wait_group<ST - 2>();
-      __syncwarp();        // the step's copies of all lanes have landed, and the slot of the step before is no longer read
-      issue(i + ST - 1);
-      const int slot = (i - i0) % ST;
-      const uint32_t live = live_s[warp][slot];
+      __syncwarp();        // the step's copies of all lanes have landed, and the stage of the step before is no longer read
+      issue(u, i - u.i0 + ST - 1, fill);
+      fill = slot;
+      const int now = slot;
+      slot = slot + 1 == ST ? 0 : slot + 1;
+      const uint32_t live = live_s[warp][now];
       if (live == 0u) continue;
-      const int t0 = token0(i);
-      const uint32_t kb = ring + slot * 2 * Cfg::kTile, vb = kb + Cfg::kTile;
-      // S = Q K^T, tokens 0..7 and 8..15
-      float x[MT][2][4];
+      const int t0 = token0(u, i);
+      const uint32_t kb = ring + now * Cfg::kStep, vb = kb + Cfg::kTile;
+      // S^T = K Q^T: tile g of 16 tokens, this lane's are l4 and l4 + 8 of each
+      float x[NR][TOK / 16][4];
 #pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
+      for (int g = 0; g < TOK / 16; ++g) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) x[mt][nt][0] = x[mt][nt][1] = x[mt][nt][2] = x[mt][nt][3] = 0.f;
-        const uint32_t krow = kb + (nt * 8 + l4) * 128;
-        if constexpr (FP8) {
+        for (int n = 0; n < NR; ++n) x[n][g][0] = x[n][g][1] = x[n][g][2] = x[n][g][3] = 0.f;
+        const uint32_t krow = kb + (g * 16 + l4) * 128;
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const uint4 v = lds128(krow + (((2 * c + u) ^ l4) << 4));
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t b0 = e4m3x2_to_f16x2(w[k] & 0xffffu), b1 = e4m3x2_to_f16x2(w[k] >> 16);
-#pragma unroll
-              for (int mt = 0; mt < MT; ++mt) mma_16816_f16(x[mt][nt], qa[mt][u * 4 + k], b0, b1);
-            }
-          }
-        } else {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const uint4 v = lds128(krow + (u >> 1) * Cfg::kHalf + (((2 * c + (u & 1)) ^ l4) << 4));
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              mma_16816_bf16(x[mt][nt], qa[mt][u * 2], v.x, v.y);
-              mma_16816_bf16(x[mt][nt], qa[mt][u * 2 + 1], v.z, v.w);
-            }
-          }
-        }
-      }
-      // logits: scales, masks
-      float kmul[2] = {1.f, 1.f}, vlog[2] = {0.f, 0.f}, vinv[2] = {1.f, 1.f};
-      if constexpr (FMT == FMT_FP8_PAGE) {
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) {
-          kmul[nt] = page_scales[warp][slot][nt];
-          const float vs = page_scales[warp][slot][2 + nt];
-          vlog[nt] = vs > 0.f ? __log2f(vs) : 0.f;
-          vinv[nt] = vs > 0.f ? 1.0f / vs : 0.f;
-        }
-      }
-      const bool all = live == 0xffffu && t0 + 15 <= pmin && (A.window <= 0 || t0 > pmax - A.window || t0 + 15 < A.sinks);
-      uint32_t pa[MT][4], pl[MT][4];
-      (void)pl;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float y = x[mt][nt][e] * cs[mt][e >> 1];
-            if constexpr (FMT == FMT_FP8_PAGE) y = fmaf(y, kmul[nt], vlog[nt]);
-            x[mt][nt][e] = y;
-          }
-        if (!all) {
-#pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = nt * 8 + 2 * c + (e & 1), tok = t0 + j, p = prow[mt][e >> 1];
-              const bool see = ((live >> j) & 1u) && tok <= p && (A.window <= 0 || tok > p - A.window || tok < A.sinks);
-              if (!see) x[mt][nt][e] = -INFINITY;
-            }
-        }
-        float mx[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float a = fmaxf(fmaxf(x[mt][0][2 * u], x[mt][0][2 * u + 1]), fmaxf(x[mt][1][2 * u], x[mt][1][2 * u + 1]));
-          a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 1));
-          mx[u] = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 2));
-        }
-        // m is the reference of the exponentials, 8 below the maximum when it was set; moved when a row has outgrown it by 14
-        // (F16 holds 2^15)
-        if (__any_sync(0xffffffffu, mx[0] > m[mt][0] + 14.f || mx[1] > m[mt][1] + 14.f)) {
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const float mn = fmaxf(m[mt][u], mx[u] - 8.f);
-            const float f = mn == m[mt][u] ? 1.f : ex2(m[mt][u] - mn);
-            m[mt][u] = mn;
-            l[mt][u] *= f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-              o[mt][j][2 * u] *= f;
-              o[mt][j][2 * u + 1] *= f;
-            }
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const float ref = m[mt][u] == -INFINITY ? 0.f : m[mt][u];
-#pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
-            const float p0 = ex2(x[mt][nt][2 * u] - ref), p1 = ex2(x[mt][nt][2 * u + 1] - ref);
-            l[mt][u] = FMT == FMT_FP8_PAGE ? fmaf(p0 + p1, vinv[nt], l[mt][u]) : l[mt][u] + (p0 + p1);
-            if constexpr (FP8) {
-              pa[mt][nt * 2 + u] = pack_f16x2(p0, p1);
-            } else {
-              const uint32_t hi = pack_bf16x2(p0, p1);
-              pa[mt][nt * 2 + u] = hi;
-              pl[mt][nt * 2 + u] = pack_bf16x2(p0 - bf16_lo(hi), p1 - bf16_hi(hi));
-            }
-          }
-        }
-      }
-      // O += P V.  Contraction index 2c, 2c + 1, 2c + 8, 2c + 9 of this lane: those tokens; column l4 of tile j: a dim of its own.
-#pragma unroll
-      for (int hv = 0; hv < Cfg::kEsz; ++hv) {
-        uint32_t w[4][4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int tok = 2 * c + (k & 1) + (k >> 1) * 8;
-          const uint4 v = lds128(vb + hv * Cfg::kHalf + tok * 128 + ((l4 ^ (tok & 7)) << 4));
-          w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
-        }
-#pragma unroll
-        for (int qd = 0; qd < 4; ++qd) {
+        for (int v = 0; v < 2 * Cfg::kEsz; ++v) {
+          const uint32_t at = krow + (v >> 1) * Cfg::kHalf + (((2 * c + (v & 1)) ^ l4) << 4);
+          const uint4 wa = lds128(at), wb = lds128(at + 8 * 128);
           if constexpr (FP8) {
-            const uint32_t a0 = __byte_perm(w[0][qd], w[1][qd], 0x5140), a1 = __byte_perm(w[0][qd], w[1][qd], 0x7362);
-            const uint32_t b0 = __byte_perm(w[2][qd], w[3][qd], 0x5140), b1 = __byte_perm(w[2][qd], w[3][qd], 0x7362);
+            const uint32_t a[4] = {wa.x, wa.y, wa.z, wa.w}, d[4] = {wb.x, wb.y, wb.z, wb.w};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t f0 = e4m3x2_to_f16x2(((k >> 1 ? a1 : a0) >> (16 * (k & 1))) & 0xffffu);
-              const uint32_t f1 = e4m3x2_to_f16x2(((k >> 1 ? b1 : b0) >> (16 * (k & 1))) & 0xffffu);
+            for (int s = 0; s < 4; ++s) {
+              uint32_t a0, a1, a2, a3;
+              e4m3x4_to_f16x4(a[s], a0, a2);
+              e4m3x4_to_f16x4(d[s], a1, a3);
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) mma_16816_f16(o[mt][qd * 4 + k], pa[mt], f0, f1);
+              for (int n = 0; n < NR; ++n) mma_16816_f16(x[n][g], a0, a1, a2, a3, qb[n][4 * v + s][0], qb[n][4 * v + s][1]);
             }
           } else {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const uint32_t f0 = __byte_perm(w[0][qd], w[1][qd], k ? 0x7632 : 0x5410);
-              const uint32_t f1 = __byte_perm(w[2][qd], w[3][qd], k ? 0x7632 : 0x5410);
+            for (int n = 0; n < NR; ++n) {
+              mma_16816_bf16(x[n][g], wa.x, wb.x, wa.y, wb.y, qb[n][2 * v][0], qb[n][2 * v][1]);
+              mma_16816_bf16(x[n][g], wa.z, wb.z, wa.w, wb.w, qb[n][2 * v + 1][0], qb[n][2 * v + 1][1]);
+            }
+          }
+        }
+      }
+      float kmul[G], vlog[G], vinv[G];
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                mma_16816_bf16(o[mt][hv * 8 + qd * 2 + k], pa[mt], f0, f1);
-                mma_16816_bf16(o[mt][hv * 8 + qd * 2 + k], pl[mt], f0, f1);
+      for (int j = 0; j < G; ++j) {
+        kmul[j] = 1.f;
+        vlog[j] = 0.f;
+        vinv[j] = 1.f;
+        if constexpr (FMT == FMT_FP8_PAGE) {
+          kmul[j] = page_scales[warp][now][j];
+          const float vs = page_scales[warp][now][G + j];
+          vlog[j] = vs > 0.f ? __log2f(vs) : 0.f;
+          vinv[j] = vs > 0.f ? __frcp_rn(vs) : 0.f;
+        }
+      }
+      if (!(live == kAllLive && t0 + TOK - 1 <= u.pmin && (A.window <= 0 || t0 > u.pmax - A.window || t0 + TOK - 1 < A.sinks))) {
+#pragma unroll
+        for (int g = 0; g < TOK / 16; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = g * 16 + (e >> 1) * 8 + l4, tok = t0 + j;
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              const int p = prow[n][e & 1];
+              const bool see = ((live >> j) & 1u) && tok <= p && (A.window <= 0 || tok > p - A.window || tok < A.sinks);
+              if (!see) x[n][g][e] = -INFINITY;
+            }
+          }
+      }
+      // y = x mul + log2 vs.  m is the reference of the exponentials: 8 below the maximum when it was set, moved when a row has
+      // outgrown it by 14 (F16 holds 2^15).  Lanes look at their own tokens; only a move needs the row's maximum.
+      float my[NR][2];                   // this lane's maxima
+      bool outgrown = false;
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          float a = -INFINITY;
+#pragma unroll
+          for (int j = 0; j < G; ++j) {
+            const float y = x[n][j / 2][(j & 1) * 2 + v];
+            if constexpr (FMT == FMT_FP8_PAGE) a = fmaxf(a, fmaf(y, fmaxf(cs[n][v] * kmul[j], 1e-37f), vlog[j]));
+            else a = fmaxf(a, y);
+          }
+          my[n][v] = FMT == FMT_FP8_PAGE ? a : a * cs[n][v];
+          outgrown |= my[n][v] > m[n][v] + 14.f;
+        }
+      if (__any_sync(0xffffffffu, outgrown)) {
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            float a = my[n][v];
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
+            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
+            const float mn = fmaxf(m[n][v], a - 8.f);
+            const float f = mn == m[n][v] ? 1.f : ex2(m[n][v] - mn);
+            m[n][v] = mn;
+            l[n][v] *= f;
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+              o[n][t][v] *= f;
+              o[n][t][2 + v] *= f;
+            }
+          }
+      }
+      uint32_t pb[NR][G], pl[FP8 ? 1 : NR][G];     // P^T: rows l4, tokens 8 j + 2 c, + 1
+      (void)pl;
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float ref[2];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) ref[v] = m[n][v] == -INFINITY ? 0.f : m[n][v];
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+          float p[2];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const float mul = FMT == FMT_FP8_PAGE ? fmaxf(cs[n][v] * kmul[j], 1e-37f) : cs[n][v];
+            p[v] = ex2(fmaf(x[n][j / 2][(j & 1) * 2 + v], mul, vlog[j] - ref[v]));
+            l[n][v] = FMT == FMT_FP8_PAGE ? fmaf(p[v], vinv[j], l[n][v]) : l[n][v] + p[v];
+          }
+          if constexpr (FP8) {
+            pb[n][j] = transpose8(pack_f16x2(p[0], p[1]));
+          } else {
+            const uint32_t hi = pack_bf16x2(p[0], p[1]);
+            pb[n][j] = transpose8(hi);
+            pl[n][j] = transpose8(pack_bf16x2(p[0] - bf16_lo(hi), p[1] - bf16_hi(hi)));
+          }
+        }
+      }
+      // O^T += V^T P^T.  Contraction: tokens 2c, 2c + 1, 2c + 8, 2c + 9 of each 16; rows: dims 16 l4 + 2 t, + 1 (e4m3) or
+      // 64 hv + 8 l4 + 2 t, + 1 (BF16) of this lane.
+#pragma unroll
+      for (int g = 0; g < TOK / 16; ++g)
+#pragma unroll
+        for (int hv = 0; hv < Cfg::kEsz; ++hv) {
+          uint32_t w[4][4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int tok = 2 * c + (k & 1) + (k >> 1) * 8;
+            const uint4 v = lds128(vb + hv * Cfg::kHalf + (g * 16 + tok) * 128 + ((l4 ^ (tok & 7)) << 4));
+            w[k][0] = v.x; w[k][1] = v.y; w[k][2] = v.z; w[k][3] = v.w;
+          }
+#pragma unroll
+          for (int qd = 0; qd < 4; ++qd) {
+            if constexpr (FP8) {
+              uint32_t f[4], h[4];
+              e4m3x4_to_f16x4(__byte_perm(w[0][qd], w[1][qd], 0x5140), f[0], f[1]);
+              e4m3x4_to_f16x4(__byte_perm(w[0][qd], w[1][qd], 0x7362), f[2], f[3]);
+              e4m3x4_to_f16x4(__byte_perm(w[2][qd], w[3][qd], 0x5140), h[0], h[1]);
+              e4m3x4_to_f16x4(__byte_perm(w[2][qd], w[3][qd], 0x7362), h[2], h[3]);
+#pragma unroll
+              for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+                  mma_16816_f16(o[n][qd * 2 + k], f[2 * k], f[2 * k + 1], h[2 * k], h[2 * k + 1], pb[n][2 * g], pb[n][2 * g + 1]);
+            } else {
+              const uint32_t f0 = __byte_perm(w[0][qd], w[1][qd], 0x5410), f1 = __byte_perm(w[0][qd], w[1][qd], 0x7632);
+              const uint32_t h0 = __byte_perm(w[2][qd], w[3][qd], 0x5410), h1 = __byte_perm(w[2][qd], w[3][qd], 0x7632);
+#pragma unroll
+              for (int n = 0; n < NR; ++n) {
+                mma_16816_bf16(o[n][hv * 4 + qd], f0, f1, h0, h1, pb[n][2 * g], pb[n][2 * g + 1]);
+                mma_16816_bf16(o[n][hv * 4 + qd], f0, f1, h0, h1, pl[n][2 * g], pl[n][2 * g + 1]);
               }
             }
           }
         }
-      }
     }
-    cp_async_wait_all();
+    // The next unit's first copies, into stages that the join below leaves alone.  (All copies of this unit that read anything were
+    // waited for in its last step.)
+    __syncwarp();
+    if (more) {
+      pids_next = pids_un;
+#pragma unroll 1
+      for (int k = 0; k < Cfg::kEarly; ++k) issue(un, k, k);
+    }
 
     // ------------------------------ the four warps' results ------------------------------
-    __syncthreads();      // the ring is free (and so is what the unit before left in shared memory)
-    float* const osm = reinterpret_cast<float*>(smem);      // [warp][row][128], 16-byte pieces permuted
-    auto piece = [](int k) { return k ^ (k >> 3); };        // of 32 pieces of a row
+    auto osm = [&](int w) { return reinterpret_cast<float*>(smem + w * Cfg::kRing + Cfg::kEarly * Cfg::kStep); };   // [row][128]
+    auto piece = [](int row, int k) { return k ^ ((row >> 1) & 3); };   // place of a row's 16-byte piece k, against bank conflicts
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
+    for (int n = 0; n < NR; ++n)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float ls = l[mt][u];
-        ls += __shfl_xor_sync(0xffffffffu, ls, 1);
-        ls += __shfl_xor_sync(0xffffffffu, ls, 2);
-        const int row = mt * 16 + u * 8 + l4;
-        if (c == 0) ml_s[warp][row] = make_float2(m[mt][u], ls);
-        float* const orow = osm + (warp * RT + row) * 128;
-        // tile j's column 2c + e is dim 16 (2c + e) + j (e4m3) or 64 (j >> 3) + 8 (2c + e) + (j & 7) (BF16)
+      for (int v = 0; v < 2; ++v) {
+        float ls = l[n][v];
+        ls += __shfl_xor_sync(0xffffffffu, ls, 4);
+        ls += __shfl_xor_sync(0xffffffffu, ls, 8);
+        ls += __shfl_xor_sync(0xffffffffu, ls, 16);
+        const int row = n * 8 + 2 * c + v;
+        if (l4 == 0) ml_s[warp][row] = make_float2(m[n][v], ls);
+        float* const orow = osm(warp) + row * 128;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const int dim = FP8 ? 16 * (2 * c + e) + j : 64 * (j >> 3) + 8 * (2 * c + e) + (j & 7);
-            *reinterpret_cast<float4*>(orow + piece(dim >> 2) * 4) =
-                make_float4(o[mt][j][2 * u + e], o[mt][j + 1][2 * u + e], o[mt][j + 2][2 * u + e], o[mt][j + 3][2 * u + e]);
-          }
-      }
-    __syncthreads();
-    const bool whole = i0 == 0 && i1 == sq.nblk;
-    const size_t slot_row = (size_t)(2 * blockIdx.x + (i0 == 0 ? 1 : 0)) * RT;
-    const float out_scale = FMT == FMT_FP8_HEAD ? A.v_scale[h] : 1.f;
-    auto write = [&](int row, int pc, float4 acc, float M, float L) {
-      const int r = r0 + row, tok = r / grp, head = h * grp + r - tok * grp;
-      const size_t at = (size_t)(sq.c0 + tok);
-      const float inv = L > 0.f ? out_scale / L : L == 0.f ? 0.f : NAN;
-      uint2 w;
-      w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
-      w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
-      *reinterpret_cast<uint2*>(A.out + (at * A.num_q_heads + head) * kHeadDim + pc * 4) = w;
-      if (pc == 0 && A.lse != nullptr)
-        A.lse[(size_t)head * A.total_q + at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-    };
-    for (int k = tid; k < nrows * 32; k += kDecThreads) {
-      const int row = k >> 5, pc = k & 31;
-      float M = -INFINITY, L = 0.f;
-#pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) M = fmaxf(M, ml_s[w][row].x);
-      const float ref = M == -INFINITY ? 0.f : M;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int w = 0; w < kDecWarps; ++w) {
-        const float2 ml = ml_s[w][row];
-        const float f = ex2(ml.x - ref);
-        const float4 v = *reinterpret_cast<const float4*>(osm + (w * RT + row) * 128 + piece(pc) * 4);
-        L = fmaf(f, ml.y, L);
-        acc.x = fmaf(f, v.x, acc.x);
-        acc.y = fmaf(f, v.y, acc.y);
-        acc.z = fmaf(f, v.z, acc.z);
-        acc.w = fmaf(f, v.w, acc.w);
-      }
-      if (whole) {
-        write(row, pc, acc, M, L);
-      } else {
-        __stcg(reinterpret_cast<float4*>(A.part_o + (slot_row + row) * 128) + pc, acc);
-        if (pc == 0) __stcg(A.part_ml + slot_row + row, make_float2(M, L));
-      }
-    }
-    if (!whole) {
-      const int w0 = (int)(unit0 / share), parts = (int)((unit0 + sq.nblk - 1) / share) - w0 + 1;
-      __threadfence();
-      __syncthreads();
-      if (tid == 0) last_s = atomicAdd(A.counters + w0, 1) == parts - 1;
-      __syncthreads();
-      if (last_s) {
-        __threadfence();
-        if (tid == 0) A.counters[w0] = 0;
-        auto row_of = [&](int u) { return (size_t)(2 * (w0 + u) + (u == 0 ? 1 : 0)) * RT; };
-        for (int k = tid; k < nrows * 32; k += kDecThreads) {
-          const int row = k >> 5, pc = k & 31;
-          float M = -INFINITY, L = 0.f;
-#pragma unroll 4
-          for (int u = 0; u < parts; ++u) M = fmaxf(M, __ldcg(A.part_ml + row_of(u) + row).x);
-          const float ref = M == -INFINITY ? 0.f : M;
-          float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-          for (int u = 0; u < parts; ++u) {
-            const float2 ml = __ldcg(A.part_ml + row_of(u) + row);
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(A.part_o + (row_of(u) + row) * 128) + pc);
-            const float f = ex2(ml.x - ref);
-            L = fmaf(f, ml.y, L);
-            acc.x = fmaf(f, v.x, acc.x);
-            acc.y = fmaf(f, v.y, acc.y);
-            acc.z = fmaf(f, v.z, acc.z);
-            acc.w = fmaf(f, v.w, acc.w);
-          }
-          write(row, pc, acc, M, L);
+        for (int t = 0; t < 8; t += 2) {
+          const int dim = FP8 ? 16 * l4 + 2 * t : 64 * (t >> 2) + 8 * l4 + 2 * (t & 3);
+          *reinterpret_cast<float4*>(orow + piece(row, dim >> 2) * 4) = make_float4(o[n][t][v], o[n][t][2 + v], o[n][t + 1][v], o[n][t + 1][2 + v]);
         }
       }
+    const float out_scale = FMT == FMT_FP8_HEAD ? A.v_scale[u.h] : 1.f;
+    // joins what the warps have put into shared memory; final: to out and lse, else to the workspace
+    auto join = [&](bool final) {
+      __syncthreads();
+      const size_t slot_row = (size_t)(2 * blockIdx.x + (u.i0 == 0 ? 1 : 0)) * RT;
+      for (int k = tid; k < u.nrows * 32; k += kDecThreads) {
+        const int row = k >> 5, pc = k & 31;
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) M = fmaxf(M, ml_s[w][row].x);
+        const float ref = M == -INFINITY ? 0.f : M;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kDecWarps; ++w) {
+          const float2 ml = ml_s[w][row];
+          const float f = ex2(ml.x - ref);
+          const float4 v = *reinterpret_cast<const float4*>(osm(w) + row * 128 + piece(row, pc) * 4);
+          L = fmaf(f, ml.y, L);
+          acc.x = fmaf(f, v.x, acc.x);
+          acc.y = fmaf(f, v.y, acc.y);
+          acc.z = fmaf(f, v.z, acc.z);
+          acc.w = fmaf(f, v.w, acc.w);
+        }
+        if (final) {
+          const int r = u.r0 + row, tok = r / grp, head = u.h * grp + r - tok * grp;
+          const size_t at = (size_t)(u.c0 + tok);
+          const float inv = L > 0.f ? out_scale / L : L == 0.f ? 0.f : NAN;
+          uint2 w;
+          w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
+          w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+          *reinterpret_cast<uint2*>(A.out + (at * A.num_q_heads + head) * kHeadDim + pc * 4) = w;
+          if (pc == 0 && A.lse != nullptr)
+            A.lse[(size_t)head * A.total_q + at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        } else {
+          __stcg(reinterpret_cast<float4*>(A.part_o + (slot_row + row) * 128) + pc, acc);
+          if (pc == 0) __stcg(A.part_ml + slot_row + row, make_float2(M, L));
+        }
+      }
+    };
+    join(u.whole);
+    if (!u.whole) {
+      __threadfence();
+      __syncthreads();
+      if (tid == 0) last_s = atomicAdd(A.counters + u.w0, 1) == u.parts - 1;
+      __syncthreads();
+      if (last_s) {
+        // All parts are in the workspace: every warp joins a quarter of them, eight rows at a time, then as above.
+        __threadfence();
+        if (tid == 0) A.counters[u.w0] = 0;
+#pragma unroll 1
+        for (int r0 = 0; r0 < u.nrows; r0 += 8) {
+          float M[8], L[8];
+          float4 acc[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            M[r] = -INFINITY;
+            L[r] = 0.f;
+            acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+#pragma unroll 2
+          for (int k = warp; k < u.parts; k += kDecWarps) {
+            const size_t row = (size_t)(2 * (u.w0 + k) + (k == 0 ? 1 : 0)) * RT + r0;
+            float4 v[8];
+            float2 ml[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const bool in = r0 + r < u.nrows;
+              ml[r] = in ? __ldcg(A.part_ml + row + r) : make_float2(-INFINITY, 0.f);
+              v[r] = in ? __ldcg(reinterpret_cast<const float4*>(A.part_o + (row + r) * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const float mn = fmaxf(M[r], ml[r].x), ref = mn == -INFINITY ? 0.f : mn;
+              const float f0 = ex2(M[r] - ref), f1 = ex2(ml[r].x - ref);
+              M[r] = mn;
+              L[r] = fmaf(f1, ml[r].y, f0 * L[r]);
+              acc[r].x = fmaf(f1, v[r].x, f0 * acc[r].x);
+              acc[r].y = fmaf(f1, v[r].y, f0 * acc[r].y);
+              acc[r].z = fmaf(f1, v[r].z, f0 * acc[r].z);
+              acc[r].w = fmaf(f1, v[r].w, f0 * acc[r].w);
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            if (lane == 0) ml_s[warp][r0 + r] = make_float2(M[r], L[r]);
+            *reinterpret_cast<float4*>(osm(warp) + (r0 + r) * 128 + piece(r0 + r, lane) * 4) = acc[r];
+          }
+        }
+        join(true);
+      }
     }
-    __syncthreads();      // shared memory is free for the next unit's copies
-    pos = unit0 + i1;
+    if (!more) return;
+    __syncthreads();      // the join's shared memory is free for the next unit's copies
+    u = un;
   }
 }
 

@@ -29,12 +29,14 @@ constexpr int64_t kMaxCacheTokens = 1ll << 30;   // positions and windows are 32
 static int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 static bool on(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
 
+template <int FMT, int NR>
+static bool set_decode_attr() {
+  return cudaFuncSetAttribute(decode_kernel<FMT, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize, DecodeCfg<FMT, NR>::kSmemBytes) ==
+         cudaSuccess;
+}
 template <int FMT>
 static bool set_decode_attrs() {
-  return cudaFuncSetAttribute(decode_kernel<FMT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, DecodeCfg<FMT>::kSmemBytes) ==
-             cudaSuccess &&
-         cudaFuncSetAttribute(decode_kernel<FMT, 2>, cudaFuncAttributeMaxDynamicSharedMemorySize, DecodeCfg<FMT>::kSmemBytes) ==
-             cudaSuccess;
+  return set_decode_attr<FMT, 1>() && set_decode_attr<FMT, 2>() && set_decode_attr<FMT, 4>();
 }
 
 extern "C" fp2_status fp2_cache_create(const fp2_cache_params* p, fp2_cache** out) {
@@ -49,6 +51,7 @@ extern "C" fp2_status fp2_cache_create(const fp2_cache_params* p, fp2_cache** ou
   if (shift > 7) return FP2_ERR_UNSUPPORTED;
   if (p->format != FP2_CACHE_BF16 && p->format != FP2_CACHE_FP8_HEAD && p->format != FP2_CACHE_FP8_PAGE)
     return FP2_ERR_UNSUPPORTED;
+  if ((int64_t)p->num_pages << shift > 0x7fffffffll) return FP2_ERR_CAPACITY;   // slots are 31-bit
   if ((int64_t)p->max_pages_per_seq << shift > kMaxCacheTokens || (int64_t)p->num_q_heads * kHeadDim > 1 << 20)
     return FP2_ERR_CAPACITY;
   fp2_cache* c = new (std::nothrow) fp2_cache();
@@ -180,6 +183,15 @@ extern "C" fp2_status fp2_cache_expand(const fp2_cache* c, const void* k, const 
                 kExpandThreads, 0, stream, a);
 }
 
+// Packed rows of a tile by the rows that a sequence has on average: its pages are read once for all of them up to 32, and
+// below that no more than twice the rows there are is paid for.
+template <int FMT>
+static fp2_status launch_decode(int64_t rows, int64_t grid, fp2_stream stream, const DecodeArgs& a) {
+  return rows <= 8    ? launch(decode_kernel<FMT, 1>, grid, kDecThreads, DecodeCfg<FMT, 1>::kSmemBytes, stream, a)
+         : rows <= 16 ? launch(decode_kernel<FMT, 2>, grid, kDecThreads, DecodeCfg<FMT, 2>::kSmemBytes, stream, a)
+                      : launch(decode_kernel<FMT, 4>, grid, kDecThreads, DecodeCfg<FMT, 4>::kSmemBytes, stream, a);
+}
+
 extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_stride, const void* k, const void* v,
                                  const int32_t* page_table, const int32_t* cu, const int32_t* lk, int32_t num_seqs,
                                  int32_t total_q, const float* ks, const float* vs, int32_t window_tokens, int32_t sink_tokens,
@@ -211,25 +223,14 @@ extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_st
   a.sinks = window_tokens > 0 ? (int32_t)std::min<int64_t>(sink_tokens, kMaxCacheTokens) : 0;
   a.scale_log2 = c->scale_log2;
   a.g = geom(c, num_seqs);
-  // two 16-row tiles per CTA where a sequence has more packed rows than one holds, on average: its pages are read once for both
-  const bool two = (int64_t)group * total_q > 16ll * num_seqs;
-  // items there can be at most (a CTA per item beyond that would find nothing)
-  const int64_t tiles = ((int64_t)group * total_q / (two ? 32 : 16) + num_seqs) * c->prm.num_kv_heads;
-  const int64_t blocks = (((int64_t)c->prm.max_pages_per_seq << c->page_shift) + kDecBlock - 1) / kDecBlock;
+  const int64_t rows = ((int64_t)group * total_q + num_seqs - 1) / num_seqs;
+  // (no more CTAs than there can be items, one of 64 tokens for a tile of 8 rows at least)
+  const int64_t tiles = ((int64_t)group * total_q / 8 + num_seqs) * c->prm.num_kv_heads;
+  const int64_t blocks = (((int64_t)c->prm.max_pages_per_seq << c->page_shift) + 63) / 64 + kDecUnitCost;
   const int64_t grid = std::min<int64_t>(c->workers, tiles * blocks);
-  void (*kernel)(DecodeArgs);
-  size_t smem;
-  if (c->prm.format == FP2_CACHE_BF16) {
-    kernel = two ? decode_kernel<FMT_BF16, 2> : decode_kernel<FMT_BF16, 1>;
-    smem = DecodeCfg<FMT_BF16>::kSmemBytes;
-  } else if (c->prm.format == FP2_CACHE_FP8_HEAD) {
-    kernel = two ? decode_kernel<FMT_FP8_HEAD, 2> : decode_kernel<FMT_FP8_HEAD, 1>;
-    smem = DecodeCfg<FMT_FP8_HEAD>::kSmemBytes;
-  } else {
-    kernel = two ? decode_kernel<FMT_FP8_PAGE, 2> : decode_kernel<FMT_FP8_PAGE, 1>;
-    smem = DecodeCfg<FMT_FP8_PAGE>::kSmemBytes;
-  }
-  return launch(kernel, grid, kDecThreads, smem, stream, a);
+  return c->prm.format == FP2_CACHE_BF16       ? launch_decode<FMT_BF16>(rows, grid, stream, a)
+         : c->prm.format == FP2_CACHE_FP8_HEAD ? launch_decode<FMT_FP8_HEAD>(rows, grid, stream, a)
+                                               : launch_decode<FMT_FP8_PAGE>(rows, grid, stream, a);
 }
 
 extern "C" fp2_status fp2_cache_read_status(const fp2_cache* c, void* workspace, int32_t* h_words, fp2_stream stream) {
