@@ -8,8 +8,9 @@
 // Work split.  The (sequence, KV head, tile of packed rows, block of tokens) items are numbered in that order, and every CTA of a
 // grid that fills the GPU takes an equal contiguous share, whatever the lengths: a long sequence is cut wherever shares end.  The
 // lengths are read on the device (a captured graph stays valid as sequences grow), so the CTAs find their shares themselves.  A
-// unit (sequence, head, tile) cut into parts leaves (O, m, l) of each in the workspace, and the CTA that arrives last joins them,
-// in the order of the shares: the result does not depend on who is last.  One launch.
+// unit (sequence, head, tile) cut into parts leaves (O, m, l) of each in the workspace; the CTA that arrives last of each group of
+// 16 parts joins these, the last of the groups these, both in the order of the shares: the result does not depend on who is
+// last.  One launch.
 //
 // A CTA is four warps, two CTAs to an SM.  Of a block each warp takes a step of kTok tokens (8 KB), which it copies into its own
 // part of shared memory (cp.async, kStages steps ahead) and attends to with its own running maximum and sum: no barrier in the
@@ -40,8 +41,11 @@ namespace fp2 {
 constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kDecCtasPerSm = 2;
-constexpr int kDecMinShare = 4;               // least share of a CTA, in blocks (kDecUnitCost included)
-constexpr int kDecUnitCost = 2;               // what a unit costs beside its blocks, in blocks
+constexpr int kDecGroup = 16;                 // parts of a unit that are joined at a time: see join_parts
+constexpr int kDecJoin = 2;                   // of these in a warp's registers
+constexpr int kDecWhole = 12;                 // units up to this long are not cut: they belong to the share that they begin in
+constexpr int kDecMinShare = 6;               // least share of a CTA, in blocks (kDecUnitCost included)
+constexpr int kDecUnitCost = 4;               // what a unit costs beside its blocks, in blocks
 
 template <int FMT, int NR>
 struct DecodeCfg {
@@ -71,9 +75,10 @@ struct DecodeArgs {
   float* lse;
   float* part_o;                // [2 grid][8 NR][128]
   float2* part_ml;              // [2 grid][8 NR]
-  int32_t* counters;            // [grid], zero between calls
+  int32_t* counters;            // [3][grid], zero between calls: parts of a unit's first group, of a later group, groups of a unit
   int* status;
   int32_t total_q, num_q_heads, group, window, sinks;
+  uint32_t group_magic;         // 2^32 / group rounded up, 0 for a group of one: see div_group
   float scale_log2;
   CacheGeom g;
 };
@@ -147,9 +152,18 @@ __device__ __forceinline__ uint4 lds128(uint32_t a) {
   return r;
 }
 
+// a / b for a >= 0, b > 0; the 64-bit division is a long routine, and seldom needed
+__device__ __forceinline__ long long div_ll(long long a, long long b) {
+  return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
+// x / group for x up to group + 32 (exact while x group < 2^32; a group has at most 2^13 heads)
+__device__ __forceinline__ int div_group(const DecodeArgs& A, int x) { return A.group_magic ? (int)__umulhi((uint32_t)x, A.group_magic) : x; }
+
 // A unit's part of this CTA: blocks i0 .. i1 - 1 of it
 struct DecodeUnit {
-  int b, h, r0, nrows;
+  int b, h, nrows;
+  int tok0, rem;               // query (of the sequence) of the first row, rows of that query in front of the tile
   int c0, first_pos, L, sb, wb0;
   int pmin, pmax;              // positions of the first and last row
   int i0, i1;
@@ -171,7 +185,7 @@ decode_kernel(DecodeArgs A) {
   __shared__ uint32_t live_s[kDecWarps][ST];               // tokens of the step that were copied
   __shared__ float2 ml_s[kDecWarps][RT];
   __shared__ long long scan_s[kDecWarps];
-  __shared__ long long found_base;
+  __shared__ long long found_base;                         // (the sequence that the share begins in, what is in front of it)
   __shared__ int found_b, last_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -181,84 +195,120 @@ decode_kernel(DecodeArgs A) {
   pdl_wait();
 
   // ------------------------------ this CTA's share ------------------------------
-  long long total = 0;
-  for (int b0 = 0; b0 < A.g.num_seqs; b0 += kDecThreads)
-    total += b0 + tid < A.g.num_seqs ? decode_seq<Cfg>(A, b0 + tid, blockIdx.x == 0).cost : 0;
+  // Costs of kDecThreads sequences from b0 on: this thread's and those in front of it; returns their sum.
+  auto scan = [&](int b0, long long& lo, long long& cost, bool report) -> long long {
+    cost = b0 + tid < A.g.num_seqs ? decode_seq<Cfg>(A, b0 + tid, report).cost : 0;
+    long long incl = cost, all = 0;
 #pragma unroll
-  for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-  if (lane == 0) scan_s[warp] = total;
-  if (tid == 0) found_b = -1;
-  __syncthreads();
-  total = 0;
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 31) scan_s[warp] = incl;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kDecWarps; ++i) total += scan_s[i];
-  const long long share = max((total + gridDim.x - 1) / gridDim.x, (long long)kDecMinShare);
+    for (int i = 0; i < kDecWarps; ++i) {
+      if (i < warp) incl += scan_s[i];
+      all += scan_s[i];
+    }
+    lo = incl - cost;
+    return all;
+  };
+  long long lo, cost, all = scan(0, lo, cost, blockIdx.x == 0);
+  long long total = all;
+  for (int b0 = kDecThreads; b0 < A.g.num_seqs; b0 += kDecThreads) {
+    long long x, y;
+    __syncthreads();
+    total += scan(b0, x, y, blockIdx.x == 0);
+  }
+  const long long share = max(div_ll(total + gridDim.x - 1, gridDim.x), (long long)kDecMinShare);
   long long pos = share * blockIdx.x;
   const long long pos_end = min(total, pos + share);
   if (pos >= pos_end) return;
   {
     long long base = 0;
-    for (int b0 = 0; b0 < A.g.num_seqs; b0 += kDecThreads) {
-      const long long cost = b0 + tid < A.g.num_seqs ? decode_seq<Cfg>(A, b0 + tid, false).cost : 0;
-      long long incl = cost;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const long long o = __shfl_up_sync(0xffffffffu, incl, d);
-        if (lane >= d) incl += o;
+    for (int b0 = 0;; b0 += kDecThreads) {   // (the first 128 sequences' numbers are here still)
+      if (b0 > 0) {
+        __syncthreads();
+        all = scan(b0, lo, cost, false);
       }
-      __syncthreads();
-      if (lane == 31) scan_s[warp] = incl;
-      __syncthreads();
-      long long all = 0;
-#pragma unroll
-      for (int i = 0; i < kDecWarps; ++i) {
-        if (i < warp) incl += scan_s[i];
-        all += scan_s[i];
-      }
-      const long long lo = base + incl - cost;
-      if (pos >= lo && pos < lo + cost) {
+      if (pos >= base + lo && pos < base + lo + cost) {
         found_b = b0 + tid;
-        found_base = lo;
+        found_base = base + lo;
       }
       base += all;
       if (base > pos) break;
     }
     __syncthreads();
   }
+  // The unit that `pos` is in: sequence, head, tile, first place.  A unit takes kDecUnitCost places in front of its blocks'.
   int b = found_b;
-  long long seq_base = found_base;
   DecodeSeq sq = decode_seq<Cfg>(A, b, false);
-  // Next unit of the share.  A unit takes kDecUnitCost places in front of its blocks' in the numbering.
+  int uh, ut;
+  long long unit0;
+  {
+    const long long unit = div_ll(pos - found_base, sq.nblk + kDecUnitCost);
+    uh = (int)div_ll(unit, sq.ntiles);
+    ut = (int)(unit - (long long)uh * sq.ntiles);
+    unit0 = found_base + unit * (sq.nblk + kDecUnitCost);
+  }
+  // Next part of a unit of the share
   auto next_unit = [&](DecodeUnit& u) -> bool {
     while (pos < pos_end) {
-      while (pos >= seq_base + sq.cost) {
-        seq_base += sq.cost;
-        sq = decode_seq<Cfg>(A, ++b, false);
-      }
       const int ulen = sq.nblk + kDecUnitCost;
-      const long long unit = (pos - seq_base) / ulen;
-      const long long unit0 = seq_base + unit * ulen;
-      u.i0 = max(0, (int)(pos - unit0) - kDecUnitCost);
-      u.i1 = max(0, (int)min((long long)ulen, pos_end - unit0) - kDecUnitCost);
-      pos = min(unit0 + ulen, pos_end);
-      if (u.i0 >= u.i1) continue;
-      u.b = b;
-      u.h = (int)(unit / sq.ntiles);
-      u.r0 = (int)(unit % sq.ntiles) * RT;
-      u.nrows = min(RT, grp * sq.Lq - u.r0);
-      u.c0 = sq.c0;
-      u.first_pos = sq.L - sq.Lq;
-      u.L = sq.L;
-      u.sb = sq.sb;
-      u.wb0 = sq.wb0;
-      u.pmin = u.first_pos + u.r0 / grp;
-      u.pmax = u.first_pos + (u.r0 + u.nrows - 1) / grp;
-      u.whole = u.i0 == 0 && u.i1 == sq.nblk;
-      u.w0 = (int)((unit0 + kDecUnitCost) / share);
-      u.parts = (int)((unit0 + ulen - 1) / share) - u.w0 + 1;
-      return true;
+      const long long unit_end = unit0 + ulen;
+      if (ulen <= kDecWhole) {
+        u.i0 = pos > unit0 ? sq.nblk : 0;
+        u.i1 = sq.nblk;
+        pos = unit_end;
+      } else {
+        u.i0 = max(0, (int)(pos - unit0) - kDecUnitCost);
+        u.i1 = max(0, (int)(min(unit_end, pos_end) - unit0) - kDecUnitCost);
+        pos = min(unit_end, pos_end);
+      }
+      const bool some = u.i0 < u.i1;
+      if (some) {
+        u.b = b;
+        u.h = uh;
+        u.c0 = sq.c0;
+        u.L = sq.L;
+        u.sb = sq.sb;
+        u.wb0 = sq.wb0;
+        u.first_pos = sq.L - sq.Lq;
+        const int r0 = ut * RT;
+        u.nrows = min(RT, grp * sq.Lq - r0);
+        u.tok0 = ut ? r0 / grp : 0;
+        u.rem = r0 - u.tok0 * grp;
+        u.pmin = u.first_pos + u.tok0;
+        u.pmax = u.pmin + div_group(A, u.rem + u.nrows - 1);
+        u.whole = u.i0 == 0 && u.i1 == sq.nblk;
+        u.w0 = blockIdx.x;
+        u.parts = 1;
+        if (!u.whole) {
+          u.w0 = (int)div_ll(unit0 + kDecUnitCost, share);
+          u.parts = (int)div_ll(unit_end - 1, share) - u.w0 + 1;
+        }
+      }
+      if (pos >= unit_end) {
+        unit0 = unit_end;
+        if (++ut == sq.ntiles) {
+          ut = 0;
+          if (++uh == heads && pos < pos_end) {
+            uh = 0;
+            do sq = decode_seq<Cfg>(A, ++b, false);
+            while (sq.cost == 0);      // (items are left: there is one)
+          }
+        }
+      }
+      if (some) return true;
     }
     return false;
+  };
+  // Row of the unit's tile -> query of the sequence and query head
+  auto row_of = [&](const DecodeUnit& u, int row, int& tok, int& head) {
+    const int x = u.rem + row, d = div_group(A, x);
+    tok = u.tok0 + d;
+    head = u.h * grp + x - d * grp;
   };
 
   // ------------------------------ copies ------------------------------
@@ -363,8 +413,8 @@ decode_kernel(DecodeArgs A) {
     int prow[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      const int r = u.r0 + min(n * 8 + l4, u.nrows - 1);
-      const int tok = r / grp, head = u.h * grp + r - tok * grp;
+      int tok, head;
+      row_of(u, min(n * 8 + l4, u.nrows - 1), tok, head);
       const uint8_t* src = A.q + (long long)(u.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2);
 #pragma unroll
       for (int s = 0; s < 8; s += 2) {
@@ -404,6 +454,14 @@ decode_kernel(DecodeArgs A) {
     DecodeUnit un;                       // the next one: known early, so that its page ids are there when this one ends
     const bool more = next_unit(un);
     const int pids_un = more ? load_pids(un, un.i0) : -1;
+    if (more && warp == 0) {             // and its queries
+#pragma unroll
+      for (int k = lane; k < 2 * RT; k += 32) {
+        int tok, head;
+        row_of(un, k >> 1, tok, head);
+        if (k >> 1 < un.nrows) prefetch_l1(A.q + (long long)(un.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2) + (k & 1) * 128);
+      }
+    }
 
     float o[NR][8][4];                   // tile t: rows 2 c, 2 c + 1 of two dims of this lane's
     float m[NR][2], l[NR][2];
@@ -617,10 +675,9 @@ decode_kernel(DecodeArgs A) {
         }
       }
     const float out_scale = FMT == FMT_FP8_HEAD ? A.v_scale[u.h] : 1.f;
-    // joins what the warps have put into shared memory; final: to out and lse, else to the workspace
-    auto join = [&](bool final) {
+    // Joins what the warps have put into shared memory.  place < 0: to out and lse; else to that row of the partial results.
+    auto join = [&](long long place) {
       __syncthreads();
-      const size_t slot_row = (size_t)(2 * blockIdx.x + (u.i0 == 0 ? 1 : 0)) * RT;
       for (int k = tid; k < u.nrows * 32; k += kDecThreads) {
         const int row = k >> 5, pc = k & 31;
         float M = -INFINITY, L = 0.f;
@@ -639,8 +696,9 @@ decode_kernel(DecodeArgs A) {
           acc.z = fmaf(f, v.z, acc.z);
           acc.w = fmaf(f, v.w, acc.w);
         }
-        if (final) {
-          const int r = u.r0 + row, tok = r / grp, head = u.h * grp + r - tok * grp;
+        if (place < 0) {
+          int tok, head;
+          row_of(u, row, tok, head);
           const size_t at = (size_t)(u.c0 + tok);
           const float inv = L > 0.f ? out_scale / L : L == 0.f ? 0.f : NAN;
           uint2 w;
@@ -650,61 +708,86 @@ decode_kernel(DecodeArgs A) {
           if (pc == 0 && A.lse != nullptr)
             A.lse[(size_t)head * A.total_q + at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
         } else {
-          __stcg(reinterpret_cast<float4*>(A.part_o + (slot_row + row) * 128) + pc, acc);
-          if (pc == 0) __stcg(A.part_ml + slot_row + row, make_float2(M, L));
+          __stcg(reinterpret_cast<float4*>(A.part_o + (place + row) * 128) + pc, acc);
+          if (pc == 0) __stcg(A.part_ml + place + row, make_float2(M, L));
         }
       }
     };
-    join(u.whole);
-    if (!u.whole) {
+    // Partial results of the unit stand at place_of(w) of the CTA w that made them: place 1 of the CTA that the unit begins in, place
+    // 0 of the others.
+    auto place_of = [&](int w) { return (long long)(2 * w + (w == u.w0 ? 1 : 0)) * RT; };
+    // Whether all n have arrived at the counter, which then starts again
+    auto arrive = [&](int32_t* counter, int n) {
       __threadfence();
       __syncthreads();
-      if (tid == 0) last_s = atomicAdd(A.counters + u.w0, 1) == u.parts - 1;
+      if (tid == 0) {
+        const bool last = atomicAdd(counter, 1) == n - 1;
+        if (last) *counter = 0;
+        last_s = last;
+      }
       __syncthreads();
-      if (last_s) {
-        // All parts are in the workspace: every warp joins a quarter of them, eight rows at a time, then as above.
-        __threadfence();
-        if (tid == 0) A.counters[u.w0] = 0;
+      if (last_s) __threadfence();
+      return last_s != 0;
+    };
+    // n partial results, those of the CTAs w, w + step ..., by warp in turn, then over the warps as above.  Eight rows at a time, of
+    // kDecJoin of them at once: all loads of that are on their way together.
+    auto join_parts = [&](int w, int step, int n, long long place) {
 #pragma unroll 1
-        for (int r0 = 0; r0 < u.nrows; r0 += 8) {
-          float M[8], L[8];
-          float4 acc[8];
+      for (int r0 = 0; r0 < u.nrows; r0 += 8) {
+        float M[8], L[8];
+        float4 acc[8];
 #pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            M[r] = -INFINITY;
-            L[r] = 0.f;
-            acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-          }
-#pragma unroll 2
-          for (int k = warp; k < u.parts; k += kDecWarps) {
-            const size_t row = (size_t)(2 * (u.w0 + k) + (k == 0 ? 1 : 0)) * RT + r0;
-            float4 v[8];
-            float2 ml[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              const bool in = r0 + r < u.nrows;
-              ml[r] = in ? __ldcg(A.part_ml + row + r) : make_float2(-INFINITY, 0.f);
-              v[r] = in ? __ldcg(reinterpret_cast<const float4*>(A.part_o + (row + r) * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              const float mn = fmaxf(M[r], ml[r].x), ref = mn == -INFINITY ? 0.f : mn;
-              const float f0 = ex2(M[r] - ref), f1 = ex2(ml[r].x - ref);
-              M[r] = mn;
-              L[r] = fmaf(f1, ml[r].y, f0 * L[r]);
-              acc[r].x = fmaf(f1, v[r].x, f0 * acc[r].x);
-              acc[r].y = fmaf(f1, v[r].y, f0 * acc[r].y);
-              acc[r].z = fmaf(f1, v[r].z, f0 * acc[r].z);
-              acc[r].w = fmaf(f1, v[r].w, f0 * acc[r].w);
-            }
-          }
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            if (lane == 0) ml_s[warp][r0 + r] = make_float2(M[r], L[r]);
-            *reinterpret_cast<float4*>(osm(warp) + (r0 + r) * 128 + piece(r0 + r, lane) * 4) = acc[r];
-          }
+        for (int r = 0; r < 8; ++r) {
+          M[r] = -INFINITY;
+          L[r] = 0.f;
+          acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
-        join(true);
+#pragma unroll 1
+        for (int k0 = warp; k0 < n; k0 += kDecWarps * kDecJoin) {
+          float4 v[kDecJoin][8];
+          float2 ml[kDecJoin][8];
+#pragma unroll
+          for (int j = 0; j < kDecJoin; ++j) {
+            const int k = k0 + j * kDecWarps;
+            const long long row = place_of(w + k * step) + r0;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const bool in = k < n && r0 + r < u.nrows;
+              ml[j][r] = in ? __ldcg(A.part_ml + row + r) : make_float2(-INFINITY, 0.f);
+              v[j][r] = in ? __ldcg(reinterpret_cast<const float4*>(A.part_o + (row + r) * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < kDecJoin; ++j)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const float mn = fmaxf(M[r], ml[j][r].x), ref = mn == -INFINITY ? 0.f : mn;
+              const float f0 = ex2(M[r] - ref), f1 = ex2(ml[j][r].x - ref);
+              M[r] = mn;
+              L[r] = fmaf(f1, ml[j][r].y, f0 * L[r]);
+              acc[r].x = fmaf(f1, v[j][r].x, f0 * acc[r].x);
+              acc[r].y = fmaf(f1, v[j][r].y, f0 * acc[r].y);
+              acc[r].z = fmaf(f1, v[j][r].z, f0 * acc[r].z);
+              acc[r].w = fmaf(f1, v[j][r].w, f0 * acc[r].w);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          if (lane == 0) ml_s[warp][r0 + r] = make_float2(M[r], L[r]);
+          *reinterpret_cast<float4*>(osm(warp) + (r0 + r) * 128 + piece(r0 + r, lane) * 4) = acc[r];
+        }
+      }
+      join(place);
+    };
+    join(u.whole ? -1 : place_of(blockIdx.x));
+    if (!u.whole) {
+      // The last CTA of a group of kDecGroup joins the group's results, the last of these the groups'.
+      const int group0 = ((int)blockIdx.x - u.w0) / kDecGroup * kDecGroup, groups = (u.parts + kDecGroup - 1) / kDecGroup;
+      const int n = min(kDecGroup, u.parts - group0);
+      // (counters by CTA: at most one unit that goes on behind it begins in a CTA, and at most one goes on into it)
+      if (arrive(A.counters + (group0 ? gridDim.x : 0) + u.w0 + group0, n)) {
+        join_parts(u.w0 + group0, 1, n, groups == 1 ? -1 : place_of(u.w0 + group0));
+        if (groups > 1 && arrive(A.counters + 2 * gridDim.x + u.w0, groups)) join_parts(u.w0, kDecGroup, groups, -1);
       }
     }
     if (!more) return;

@@ -77,7 +77,7 @@ extern "C" fp2_status fp2_cache_create(const fp2_cache_params* p, fp2_cache** ou
   }
   c->workers = std::max(sms, 1) * kDecCtasPerSm;
   int64_t o = 1024;                                        // status block
-  c->ws_counters = o; o += up(4 * (int64_t)c->workers, 1024);
+  c->ws_counters = o; o += up(12 * (int64_t)c->workers, 1024);
   c->ws_part_ml = o;  o += up(2ll * c->workers * kMaxDecodeTileRows * 8, 1024);
   c->ws_part_o = o;   o += 2ll * c->workers * kMaxDecodeTileRows * kHeadDim * 4;
   c->ws_bytes = o;
@@ -219,6 +219,7 @@ extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_st
   a.counters = (int32_t*)(ws + c->ws_counters);
   a.status = (int*)ws;
   a.total_q = total_q; a.num_q_heads = c->prm.num_q_heads; a.group = group;
+  a.group_magic = group > 1 ? (uint32_t)(((1ull << 32) + group - 1) / group) : 0u;
   a.window = (int32_t)std::min<int64_t>(window_tokens, kMaxCacheTokens);   // (no position is that far away)
   a.sinks = window_tokens > 0 ? (int32_t)std::min<int64_t>(sink_tokens, kMaxCacheTokens) : 0;
   a.scale_log2 = c->scale_log2;
