@@ -319,7 +319,7 @@ fp2_status fp2_cache_append(const fp2_cache* cache, const void* k_new, const voi
 
 /* An 8-bit cache as BF16 pages (code times scale, rounded once), for stage calls of a BF16 plan: prefill chunks behind a
  * prefix that is kept in 8 bits, or block selection on it.  Page j of sequence b goes to page out_page_table[b][j] of k_out /
- * v_out, BF16 [out_num_pages, page_size, num_kv_heads, 128], 16-byte aligned; out_page_table has the shape of page_table, and
+ * v_out, BF16 [out_num_pages, page_size, num_kv_heads, 128], 32-byte aligned; out_page_table has the shape of page_table, and
  * no page may occur in it twice.  Rows of a last page behind the sequence's end become zero.  FP2_ERR_UNSUPPORTED for BF16
  * caches.  One kernel on `stream`. */
 fp2_status fp2_cache_expand(const fp2_cache* cache, const void* k_cache, const void* v_cache, const int32_t* page_table,

@@ -44,7 +44,7 @@ constexpr int kDecCtasPerSm = 2;
 constexpr int kDecGroup = 16;                 // parts of a unit that are joined at a time: see join_parts
 constexpr int kDecJoin = 2;                   // of these in a warp's registers
 constexpr int kDecWhole = 12;                 // units up to this long are not cut: they belong to the share that they begin in
-constexpr int kDecMinShare = 6;               // least share of a CTA, in blocks (kDecUnitCost included)
+constexpr int kDecMinShare = 5;               // least share of a CTA, in blocks (kDecUnitCost included)
 constexpr int kDecUnitCost = 4;               // what a unit costs beside its blocks, in blocks
 
 template <int FMT, int NR>

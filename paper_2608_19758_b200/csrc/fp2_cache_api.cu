@@ -148,11 +148,14 @@ extern "C" fp2_status fp2_cache_append(const fp2_cache* c, const void* k_new, co
   a.k_scale = ks; a.v_scale = vs;
   a.status = (int*)workspace;
   a.total_new = total_new;
-  a.slots = (long long)(total_new >> c->page_shift) + 2ll * num_seqs;   // see append_slot0
   a.g = geom(c, num_seqs);
-  const int wpi = std::max(1, c->prm.page_size / 16);
-  const int64_t per_cta = kAppendThreads / 32 / wpi;
-  const int64_t grid = (a.slots * 2 * c->prm.num_kv_heads + per_cta - 1) / per_cta;
+  const int64_t slots = (int64_t)(total_new >> c->page_shift) + 2ll * num_seqs;   // see append_slot0
+  // A CTA per page, or up to one per turn of its warps as long as there are no more than 18 CTAs per SM: four are resident, and
+  // with few waves of long ones the last wave leaves the chip idle.  41392 tokens, 64 / 128 a page, up to 4 / 9 / 18 / 27 per SM:
+  // 55.2 / 48.6 / 46.6 / 49.9 us, 71.2 / 51.3 / 48.8 / 50.0.
+  const int64_t turns = (2ll * c->prm.num_kv_heads * std::max(1, c->prm.page_size / 16) + 7) / 8;
+  a.split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(turns, 18 * (c->workers / kDecCtasPerSm) / slots));
+  const int64_t grid = slots * a.split;
   auto kernel = c->prm.format == FP2_CACHE_BF16 ? cache_append_kernel<FMT_BF16>
                 : c->prm.format == FP2_CACHE_FP8_HEAD ? cache_append_kernel<FMT_FP8_HEAD> : cache_append_kernel<FMT_FP8_PAGE>;
   return launch(kernel, grid, kAppendThreads, 0, stream, a);
@@ -167,7 +170,7 @@ extern "C" fp2_status fp2_cache_expand(const fp2_cache* c, const void* k, const 
   if (s != FP2_OK) return s;
   if (!out_page_table || out_num_pages < 0) return FP2_ERR_INVALID_ARG;
   if (num_seqs == 0) return FP2_OK;
-  if (!on(k_out, 16) || !on(v_out, 16)) return FP2_ERR_INVALID_ARG;
+  if (!on(k_out, 32) || !on(v_out, 32)) return FP2_ERR_INVALID_ARG;
   if ((s = check_device(c)) != FP2_OK) return s;
   ExpandArgs a;
   a.k_cache = (const uint8_t*)k; a.v_cache = (const uint8_t*)v;

@@ -49,10 +49,20 @@ __device__ __forceinline__ float page_scale_for(uint32_t amax_bits) {
 // Number of page slots reserved in front of sequence b's: its n new tokens touch at most n / p + 2 pages.
 __device__ __forceinline__ long long append_slot0(int cu, int b, int shift) { return (long long)(cu >> shift) + 2ll * b; }
 
-// One item = the new tokens of one (page, KV head, K | V); rows of a page in groups of 16 to a warp, so that a warp keeps all it
+// Maximum of the magnitudes of BF16 pairs (a NaN loses against a number; NaN against NaN stays)
+__device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b & 0x7fff7fffu));
+  return d;
+}
+
+// An item = the new tokens of one (page, KV head, K | V); rows of a page in groups of 16 to a warp, so that a warp keeps all it
 // reads in registers between the maximum and the rounding: the tokens are read once.  16 lanes to a row (16 bytes of BF16 in, 8
-// of e4m3 out each), eight rows in flight per lane.  A CTA of eight warps holds 8 / W items, W = warps per page.
-// Bound by memory (2 bytes read and 1 written per element) for prompts, by launch and load latency for single tokens.
+// of e4m3 out each), eight rows in flight per lane.  A CTA looks its page up once and goes over the page's heads (or, when there
+// are few pages, `split` CTAs share them): what a warp does is wait, for the lengths, then for tokens and page id together, so it
+// should not wait again for each head.  41392 tokens, 8 heads, 64 a page: 59.6 us with a CTA and its look-ups for every 16 KB,
+// APPEND_US so (4.3, APPEND_BW TB/s).  Bound by memory for prompts (2 bytes read and 1 written per element), by launch and load
+// latency for single tokens.
 constexpr int kAppendThreads = 256;
 
 struct AppendArgs {
@@ -63,153 +73,170 @@ struct AppendArgs {
   float *k_scale, *v_scale;
   int* status;
   int32_t total_new;
-  long long slots;                    // page slots of all sequences
+  int32_t split;                      // CTAs per page slot
   CacheGeom g;
 };
 
 template <int FMT>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, 4)
 cache_append_kernel(AppendArgs A) {
   constexpr int kRows = 16;           // rows per warp
-  __shared__ uint32_t amax_s[kAppendThreads / 32];
+  constexpr int kWarps = kAppendThreads / 32;
+  __shared__ uint32_t amax_s[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_trigger();
   pdl_wait();
   const int shift = A.g.page_shift, ps = 1 << shift, heads = A.g.num_kv_heads;
   const int wpi = ps > kRows ? ps / kRows : 1;             // warps per item: 1, 2, 4 or 8
   const int part = warp % wpi;
-  const long long item = (long long)blockIdx.x * (kAppendThreads / 32 / wpi) + warp / wpi;
-  const int h = (int)(item % heads);
-  const bool is_v = (item / heads) & 1;
-  const long long slot = item / (2 * heads);
-  bool active = slot < A.slots;
+  const long long slot = blockIdx.x / A.split;
 
-  // sequence of the slot: the last one whose first slot is not behind it
-  int b = -1;
-  if (active) {
-    for (int base = 0; base < A.g.num_seqs; base += 32) {
-      const int i = base + lane;
-      const bool le = i < A.g.num_seqs && append_slot0(A.cu[i], i, shift) <= slot;
-      const unsigned bal = __ballot_sync(0xffffffffu, le);
-      b += __popc(bal);
-      if (bal != 0xffffffffu) break;
-    }
-    active = b >= 0;
+  // sequence of the slot: the last one whose first slot is not behind it; 32-way search
+  int b = 0, n = A.g.num_seqs;
+  while (n > 32) {
+    const int stride = (n + 31) / 32, i = lane * stride;
+    const unsigned bal = __ballot_sync(0xffffffffu, i < n && append_slot0(A.cu[b + min(i, n - 1)], b + i, shift) <= slot);
+    const int skip = max(0, __popc(bal) - 1) * stride;     // (offsets that fall: any sequence)
+    b += skip;
+    n = min(stride, n - skip);
   }
-  int first = 0, end = 0, c0 = 0, page_tok = 0, pid = 0;
-  if (active) {
-    c0 = A.cu[b];
-    const int c1 = A.cu[b + 1], L = A.lk[b], n = c1 - c0;
-    const bool fits = c0 >= 0 && c1 >= c0 && c1 <= A.total_new && L >= n && L <= ((long long)A.g.max_pages << shift);
-    if (!fits && lane == 0) atomicOr(A.status + kCacheStBad, kBadLength);
-    first = L - n;
-    end = L;
-    const long long page = (first >> shift) + (slot - append_slot0(c0, b, shift));
-    active = fits && n > 0 && page >= (first >> shift) && page <= ((L - 1) >> shift);   // (offsets that fall: any slot)
-    if (active) {
-      page_tok = (int)page << shift;
-      pid = A.page_table[(size_t)b * A.g.max_pages + page];
-      if (pid < 0 || pid >= A.g.num_pages) {
-        if (lane == 0) atomicOr(A.status + kCacheStBad, kBadPage);
-        active = false;
-      }
-    }
+  int c0, c1, L;
+  {
+    const int i = b + min(lane, n - 1);
+    const int x0 = A.cu[i], x1 = A.cu[i + 1], l = A.lk[i];
+    const unsigned bal = __ballot_sync(0xffffffffu, lane < n && append_slot0(x0, i, shift) <= slot);
+    const int who = max(0, __popc(bal) - 1);
+    b += who;
+    c0 = __shfl_sync(0xffffffffu, x0, who);
+    c1 = __shfl_sync(0xffffffffu, x1, who);
+    L = __shfl_sync(0xffffffffu, l, who);
   }
-  const uint8_t* src = is_v ? A.v_new : A.k_new;
-  uint8_t* cache = is_v ? A.v_cache : A.k_cache;
-  constexpr int esz = FMT == FMT_BF16 ? 2 : 1;
-  const int col = lane & 15, half = lane >> 4;
-  const int row0 = part * kRows + half;                  // this lane's rows of the page: row0 + 2 i
-  auto out_at = [&](int row) {
-    return cache + (((size_t)pid * ps + row) * heads + h) * (kHeadDim * esz) + col * (8 * esz);
-  };
-  uint4 x[kRows / 2];
-  uint32_t live = 0;
-  if (active) {
-#pragma unroll
-    for (int i = 0; i < kRows / 2; ++i) {
-      const int row = row0 + 2 * i, tok = page_tok + row;
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (row < ps && tok >= first && tok < end) {
-        live |= 1u << i;
-        x[i] = *reinterpret_cast<const uint4*>(src + (long long)(c0 + tok - first) * A.stride_bytes + h * (kHeadDim * 2) + col * 16);
-      }
-    }
-  }
-  if constexpr (FMT == FMT_BF16) {
-    if (!active) return;
-#pragma unroll
-    for (int i = 0; i < kRows / 2; ++i)
-      if ((live >> i) & 1u) *reinterpret_cast<uint4*>(out_at(row0 + 2 * i)) = x[i];
+  if (!(c0 >= 0 && c1 >= c0 && c1 <= A.total_new && L >= c1 - c0 && L <= ((long long)A.g.max_pages << shift))) {
+    if (threadIdx.x == 0) atomicOr(A.status + kCacheStBad, kBadLength);
     return;
   }
-  float scale = 0.f;
-  if constexpr (FMT == FMT_FP8_HEAD) {
-    if (!active) return;
-    scale = (is_v ? A.v_scale : A.k_scale)[h];
-  } else {
-    float* const where = (is_v ? A.v_scale : A.k_scale) + (size_t)pid * heads + h;
-    const bool keeps = active && first > page_tok;        // rows in front of the new ones are live
-    const float before = keeps ? *where : 0.f;
-    // maximum of the finite magnitudes, as BF16 bits (ordered like integers)
-    uint32_t amax = 0;
-    if (active) {
-#pragma unroll
-      for (int i = 0; i < kRows / 2; ++i) {
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t lo = w[k] & 0x7fffu, hi = (w[k] >> 16) & 0x7fffu;
-          amax = max(amax, lo < 0x7f80u ? lo : 0u);
-          amax = max(amax, hi < 0x7f80u ? hi : 0u);
-        }
-      }
-    }
-    amax = __reduce_max_sync(0xffffffffu, amax);
-    if (wpi > 1) {   // (the same for the whole CTA)
-      if (lane == 0) amax_s[warp] = amax;
-      __syncthreads();
-      for (int i = 0; i < wpi; ++i) amax = max(amax, amax_s[warp - part + i]);
-    }
-    if (!active) return;
-    scale = fmaxf(page_scale_for(amax), before);
-    if (keeps && scale > before) {   // earlier rows of the page to the larger scale (a power of two then)
-      const float inv = 1.0f / scale;
-#pragma unroll 1
-      for (int i = 0; i < kRows / 2; ++i) {
-        const int row = row0 + 2 * i;
-        if (row >= ps || page_tok + row >= first) break;
-        uint2* const p = reinterpret_cast<uint2*>(out_at(row));
-        const uint2 old = *p;
-        uint32_t o[2];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t w = k ? old.y : old.x;
-          const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(w & 0xffffu)), c = f16x2_to_float2(e4m3x2_to_f16x2(w >> 16));
-          o[k] = pack_e4m3x2(a.x * before * inv, a.y * before * inv) | pack_e4m3x2(c.x * before * inv, c.y * before * inv) << 16;
-        }
-        *p = make_uint2(o[0], o[1]);
-      }
-    }
-    // every warp of the item has read the old scale before the barrier above, or is the only one
-    if (part == 0 && lane == 0) *where = scale;
-  }
-  // (a scale that a caller put there need not be a power of two; a product with the reciprocal would then round twice)
-  const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0u && scale >= 0x1p-126f && scale <= 0x1p126f;
-  const float inv = 1.0f / scale;
+  const int first = L - (c1 - c0);
+  const long long page = (first >> shift) + (slot - append_slot0(c0, b, shift));
+  if (c1 == c0 || page < (first >> shift) || page > ((L - 1) >> shift)) return;
+  const int page_tok = (int)page << shift;
+  const int pid = A.page_table[(size_t)b * A.g.max_pages + page];
+  constexpr int esz = FMT == FMT_BF16 ? 2 : 1;
+  const int col = lane & 15, half = lane >> 4;
+  const int row0 = part * kRows + half;                    // this lane's rows of the page: row0 + 2 i
+  uint32_t live = 0;
 #pragma unroll
   for (int i = 0; i < kRows / 2; ++i) {
-    if (!((live >> i) & 1u)) continue;
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    uint32_t o[4];
-    if (pow2) {
+    const int row = row0 + 2 * i, tok = page_tok + row;
+    live |= (row < ps && tok >= first && tok < L ? 1u : 0u) << i;
+  }
+  const long long tok_off = (long long)(c0 + page_tok + row0 - first) * A.stride_bytes + col * 16;
+  const bool keeps = first > page_tok;                     // rows in front of the new ones are live
+  const int items = 2 * heads, per_turn = kWarps / wpi;    // (the same number of turns for all warps: there is a barrier inside)
+  for (int item0 = (int)(blockIdx.x % A.split) * per_turn; item0 < items; item0 += A.split * per_turn) {
+    const int item = item0 + warp / wpi;
+    const bool active = item < items;
+    const bool is_v = item >= heads;
+    const int h = is_v ? item - heads : item;
+    const uint8_t* src = (is_v ? A.v_new : A.k_new) + tok_off + h * (kHeadDim * 2);
+    uint4 x[kRows / 2];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = pack_e4m3x2(bf16_lo(w[k]) * inv, bf16_hi(w[k]) * inv);
-    } else {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = pack_e4m3x2(__fdiv_rn(bf16_lo(w[k]), scale), __fdiv_rn(bf16_hi(w[k]), scale));
+    for (int i = 0; i < kRows / 2; ++i) {
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (active && ((live >> i) & 1u)) x[i] = *reinterpret_cast<const uint4*>(src + 2 * i * A.stride_bytes);
     }
-    *reinterpret_cast<uint2*>(out_at(row0 + 2 * i)) = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+    if (pid < 0 || pid >= A.g.num_pages) {                 // (looked at as late as this: the tokens need not wait for it)
+      if (threadIdx.x == 0) atomicOr(A.status + kCacheStBad, kBadPage);
+      return;
+    }
+    uint8_t* const out = (is_v ? A.v_cache : A.k_cache) + (((size_t)pid * ps + row0) * heads + h) * (kHeadDim * esz) + col * (8 * esz);
+    const size_t row_step = (size_t)2 * heads * (kHeadDim * esz);
+    if constexpr (FMT == FMT_BF16) {
+      if (!active) continue;
+#pragma unroll
+      for (int i = 0; i < kRows / 2; ++i)
+        if ((live >> i) & 1u) *reinterpret_cast<uint4*>(out + i * row_step) = x[i];
+      continue;
+    }
+    float scale = 1.f;
+    if constexpr (FMT == FMT_FP8_HEAD) {
+      if (!active) continue;
+      scale = (is_v ? A.v_scale : A.k_scale)[h];
+    } else {
+      float* const where = (is_v ? A.v_scale : A.k_scale) + (size_t)pid * heads + h;
+      const float before = active && keeps ? *where : 0.f;
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < kRows / 2; ++i) m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(m, x[i].x), x[i].y), x[i].z), x[i].w);
+      uint32_t amax = max(m & 0xffffu, m >> 16);
+      if (__any_sync(0xffffffffu, amax >= 0x7f80u)) {      // an infinity, or nothing but NaN: the finite ones count
+        amax = 0;
+#pragma unroll
+        for (int i = 0; i < kRows / 2; ++i) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = w[k] & 0x7fffu, hi = (w[k] >> 16) & 0x7fffu;
+            amax = max(amax, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+          }
+        }
+      }
+      amax = __reduce_max_sync(0xffffffffu, amax);
+      if (wpi > 1) {   // (the same for the whole CTA)
+        __syncthreads();                                   // (the turn before has been read)
+        if (lane == 0) amax_s[warp] = amax;
+        __syncthreads();
+        for (int i = 0; i < wpi; ++i) amax = max(amax, amax_s[warp - part + i]);
+      }
+      if (!active) continue;
+      scale = fmaxf(page_scale_for(amax), before);
+      if (keeps && scale > before) {   // earlier rows of the page to the larger scale (a power of two then)
+        const float inv = 1.0f / scale;
+#pragma unroll 1
+        for (int i = 0; i < kRows / 2; ++i) {
+          const int row = row0 + 2 * i;
+          if (row >= ps || page_tok + row >= first) break;
+          uint2* const p = reinterpret_cast<uint2*>(out + i * row_step);
+          const uint2 old = *p;
+          uint32_t o[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const uint32_t w = k ? old.y : old.x;
+            const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(w & 0xffffu)), c = f16x2_to_float2(e4m3x2_to_f16x2(w >> 16));
+            o[k] = pack_e4m3x2(a.x * before * inv, a.y * before * inv) | pack_e4m3x2(c.x * before * inv, c.y * before * inv) << 16;
+          }
+          *p = make_uint2(o[0], o[1]);
+        }
+      }
+      // every warp of the item has read the old scale before the barrier above, or is the only one
+      if (part == 0 && lane == 0) *where = scale;
+    }
+    // A power of two divides exactly.  Another scale (a caller's): the quotient lies between the products with a reciprocal rounded
+    // down and one rounded up, 2^-21 each way; where both round to the same e4m3 value so does it, and else it is divided.
+    const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0u, usual = scale >= 0x1p-100f && scale <= 0x1p126f;
+    const float inv = 1.0f / scale, inv_lo = inv * (1.f - 0x1p-21f), inv_hi = inv * (1.f + 0x1p-21f);
+    auto quantise = [&](uint32_t w, float f) { return pack_e4m3x2(bf16_lo(w) * f, bf16_hi(w) * f); };
+#pragma unroll
+    for (int i = 0; i < kRows / 2; ++i) {
+      if (!((live >> i) & 1u)) continue;
+      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      uint32_t o[4];
+      if (pow2 && usual) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = quantise(w[k], inv);
+      } else {
+        uint32_t differ = usual ? 0u : 1u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          o[k] = quantise(w[k], inv_lo);
+          differ |= o[k] ^ quantise(w[k], inv_hi);
+        }
+        if (differ) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = pack_e4m3x2(__fdiv_rn(bf16_lo(w[k]), scale), __fdiv_rn(bf16_hi(w[k]), scale));
+        }
+      }
+      *reinterpret_cast<uint2*>(out + i * row_step) = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
+    }
   }
 }
 
@@ -217,6 +244,14 @@ cache_append_kernel(AppendArgs A) {
 // one group of up to 16 rows of a page, all heads, K or V: consecutive 16-byte pieces to consecutive threads.  Bound by memory:
 // one byte read and two written per element.
 constexpr int kExpandThreads = 256;
+constexpr int kExpandBatch = 4;       // pieces of a thread on their way at a time
+
+// whole sectors: 32 bytes per thread and instruction
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&r)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+               "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
 
 struct ExpandArgs {
   const uint8_t *k_cache, *v_cache;
@@ -273,24 +308,31 @@ cache_expand_kernel(ExpandArgs A) {
       uint8_t* dst = (is_v ? A.v_out : A.k_out) + (((size_t)oid << shift) + row0) * heads * (kHeadDim * 2);
       const float* scale = (is_v ? A.v_scale : A.k_scale) + (FMT == FMT_FP8_PAGE ? (size_t)pid * heads : 0);
       const long long left = (long long)Lb - (page << shift) - row0;   // live rows of the group, all of them if more
-      for (int c = threadIdx.x; c < pieces; c += kExpandThreads) {
-        const int hr = c >> 3;                            // row * heads + head
-        const int row = hr / heads, head = hr - row * heads;
-        uint32_t o[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (row < left) {
-          const uint4 v = *reinterpret_cast<const uint4*>(src + (size_t)c * 16);
-          const float s = scale[head];
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      for (int c0 = threadIdx.x; c0 < pieces; c0 += kExpandThreads * kExpandBatch) {
+        uint4 v[kExpandBatch];
+        float s[kExpandBatch];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(w[k] & 0xffffu)), d = f16x2_to_float2(e4m3x2_to_f16x2(w[k] >> 16));
-            o[2 * k] = pack_bf16x2(a.x * s, a.y * s);
-            o[2 * k + 1] = pack_bf16x2(d.x * s, d.y * s);
-          }
+        for (int k = 0; k < kExpandBatch; ++k) {
+          const int c = c0 + k * kExpandThreads, hr = c >> 3;     // row * heads + head
+          const int row = hr / heads;
+          const bool in = c < pieces && row < left;
+          v[k] = in ? *reinterpret_cast<const uint4*>(src + (size_t)c * 16) : make_uint4(0, 0, 0, 0);
+          s[k] = in ? scale[hr - row * heads] : 0.f;
         }
-        uint4* p = reinterpret_cast<uint4*>(dst + (size_t)c * 32);
-        p[0] = make_uint4(o[0], o[1], o[2], o[3]);
-        p[1] = make_uint4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+        for (int k = 0; k < kExpandBatch; ++k) {
+          const int c = c0 + k * kExpandThreads;
+          if (c >= pieces) break;
+          const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+          uint32_t o[8];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(w[j] & 0xffffu)), d = f16x2_to_float2(e4m3x2_to_f16x2(w[j] >> 16));
+            o[2 * j] = pack_bf16x2(a.x * s[k], a.y * s[k]);
+            o[2 * j + 1] = pack_bf16x2(d.x * s[k], d.y * s[k]);
+          }
+          st_global_32(dst + (size_t)c * 32, o);
+        }
       }
     }
     base += total;

@@ -87,7 +87,7 @@ def test_calls_refuse_bad_arguments_before_they_look_for_a_device(fmt):
         assert _expand(lib, h) == 2      # BF16 pages already
     else:
         assert _expand(lib, h) == 4
-        for kw in common + [dict(ko=None), dict(vo=None), dict(ko=4104), dict(vo=4104), dict(opt=None), dict(pages=-1)]:
+        for kw in common + [dict(ko=None), dict(vo=None), dict(ko=4112), dict(vo=4112), dict(opt=None), dict(pages=-1)]:
             assert _expand(lib, h, **kw) == 1, kw
     # nothing to do: fine without a device, and without data
     assert _append(lib, h, total=0, k_new=None, v_new=None) == 0 and _append(lib, h, ns=0) == 0
