@@ -311,7 +311,7 @@ class Cache:
         n = C.c_int64()
         _check(lib.fp2_cache_sizes(h, C.byref(n)), "fp2_cache_sizes")
         self.workspace_bytes = n.value
-        self._device = torch.device("cuda", torch.cuda.current_device()) if torch.cuda.is_available() else None
+        self._device = torch.cuda.current_device() if torch.cuda.is_available() else -1
         p = self.params
         self._fp8 = p.format != CACHE_BF16
         self._pool = (p.num_pages, p.page_size, p.num_kv_heads, p.head_dim)
@@ -334,19 +334,21 @@ class Cache:
         ks, vs = (torch.ones(self._scales, dtype=torch.float32, device=device) for _ in "kv")
         return k, v, ks, vs
 
-    def _check_pages(self, where, device, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, num_seqs, workspace):
-        if self._device is not None and device != self._device:
-            raise Fp2Error(1, f"{where}: tensors on {device}, the cache was made for {self._device}")
-        kinds = _E4M3 if self._fp8 else _BF16
-        _want(where, device, k_cache, kinds, self._pool)
-        _want(where, device, v_cache, kinds, self._pool)
-        if self._scales is not None:
-            _want(where, device, k_scale, _F32, self._scales)
-            _want(where, device, v_scale, _F32, self._scales)
-        _want(where, device, page_table, _I32, (num_seqs, self.params.max_pages_per_seq))
-        _want(where, device, seqlens_k, _I32, (num_seqs,))
-        if workspace.numel() < self.workspace_bytes or workspace.device != device:
-            raise Fp2Error(1, f"{where}: workspace too small or on another device")
+    def _check_pages(self, where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, num_seqs, workspace):
+        dev = self._device
+        if self._fp8:
+            _want(where, dev, k_cache, _E4M3, self._pool)
+            _want(where, dev, v_cache, _E4M3, self._pool)
+            _want(where, dev, k_scale, _F32, self._scales)
+            _want(where, dev, v_scale, _F32, self._scales)
+        else:
+            _want(where, dev, k_cache, _BF16, self._pool)
+            _want(where, dev, v_cache, _BF16, self._pool)
+        _want(where, dev, page_table, _I32, (num_seqs, self.params.max_pages_per_seq))
+        _want(where, dev, seqlens_k, _I32, (num_seqs,))
+        if workspace.numel() < self.workspace_bytes or workspace.get_device() != dev:
+            raise Fp2Error(1, f"{where}: workspace too small or not on device {dev}")
+        return dev
 
     def close(self):
         if getattr(self, "handle", None):
@@ -363,43 +365,45 @@ class Cache:
 _E4M3, _BF16, _F32, _I32 = (torch.uint8, torch.float8_e4m3fn), (torch.bfloat16,), (torch.float32,), (torch.int32,)
 
 
-def _want(where, device, t, dtypes, shape):
-    """The C ABI sees addresses only: what a tensor must be for the address to mean what the call takes it for."""
-    if t is None or t.dtype not in dtypes or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+def _want(where, dev, t, dtypes, shape):
+    """The C ABI sees addresses only: what a tensor must be for the address to mean what the call takes it for.  `dev`: the device's
+    number, -1 where there is none (host memory, which no call then gets to read)."""
+    if t is None or t.dtype not in dtypes or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}"
-        raise Fp2Error(1, f"{where}: wanted contiguous {dtypes[0]} {shape} on {device}, got {got}")
+        raise Fp2Error(1, f"{where}: wanted contiguous {dtypes[0]} {shape} on device {dev}, got {got}")
 
 
-def _rows(where, device, t, heads):
+def _rows(where, dev, t, heads):
     """Token stride of a BF16 [tokens, heads, 128] tensor whose tokens may lie apart (a slice of a fused projection)."""
-    if t.dtype != torch.bfloat16 or t.dim() != 3 or t.shape[1:] != (heads, 128) or t.device != device or \
-            t.stride(2) != 1 or (heads > 1 and t.stride(1) != 128):
-        raise Fp2Error(1, f"{where}: wanted BF16 [tokens, {heads}, 128] on {device}, heads next to each other, got {t.dtype} "
-                          f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else heads * 128
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != 128 or t.get_device() != dev or \
+            stride[2] != 1 or (heads > 1 and stride[1] != 128):
+        raise Fp2Error(1, f"{where}: wanted BF16 [tokens, {heads}, 128] on device {dev}, heads next to each other, got {t.dtype} "
+                          f"{tuple(shape)} on {t.device}, strides {stride}")
+    return stride[0] if shape[0] > 1 else heads * 128
 
 
 def fp2_cache_append(cache: Cache, k_new, v_new, page_table, cu_seqlens_new, seqlens_k, k_cache, v_cache, k_scale, v_scale,
                      workspace, stream=None):
     """Writes the keys and values of new tokens into their pages (quantised where the cache holds 8 bits; FP8_PAGE caches get
     the pages' scales too).  seqlens_k: tokens in the cache after the call."""
-    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_cache_append"
-    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    ns, where = seqlens_k.shape[0], "fp2_cache_append"
+    dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, cu_seqlens_new, _I32, (ns + 1,))
     heads = cache.params.num_kv_heads
-    stride = _rows(where, dev, k_new, heads)
-    if _rows(where, dev, v_new, heads) != stride or v_new.shape[0] != k_new.shape[0]:
+    stride, total = _rows(where, dev, k_new, heads), k_new.shape[0]
+    if _rows(where, dev, v_new, heads) != stride or v_new.shape[0] != total:
         raise Fp2Error(1, f"{where}: k_new and v_new differ in tokens or strides")
     _check(load().fp2_cache_append(cache.handle, _ptr(k_new), _ptr(v_new), stride, _ptr(page_table), _ptr(cu_seqlens_new),
-                                   _ptr(seqlens_k), ns, k_new.shape[0], _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
+                                   _ptr(seqlens_k), ns, total, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
                                    _ptr(v_scale), _ptr(workspace), _stream(stream)), where)
 
 
 def fp2_cache_expand(cache: Cache, k_cache, v_cache, page_table, seqlens_k, k_scale, v_scale, k_out, v_out, out_page_table,
                      workspace, stream=None):
     """An 8-bit cache as BF16 pages [out_num_pages, page_size, num_kv_heads, 128] for stage calls of a BF16 plan."""
-    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_cache_expand"
-    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    ns, where = seqlens_k.shape[0], "fp2_cache_expand"
+    dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, out_page_table, _I32, tuple(page_table.shape))
     pool = (k_out.shape[0],) + cache._pool[1:]
     _want(where, dev, k_out, _BF16, pool)
@@ -412,8 +416,8 @@ def fp2_cache_expand(cache: Cache, k_cache, v_cache, page_table, seqlens_k, k_sc
 def fp2_decode(cache: Cache, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, k_scale, v_scale, out, lse, workspace,
                window_tokens: int = 0, sink_tokens: int = 0, stream=None):
     """Attention of the newest few tokens of every sequence over its pages, with an optional sliding window and sinks."""
-    ns, dev, where = seqlens_k.shape[0], k_cache.device, "fp2_decode"
-    cache._check_pages(where, dev, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
+    ns, where = seqlens_k.shape[0], "fp2_decode"
+    dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, cu_seqlens_q, _I32, (ns + 1,))
     heads, total_q = cache.params.num_q_heads, q.shape[0]
     stride = _rows(where, dev, q, heads)
