@@ -221,15 +221,29 @@ __device__ __forceinline__ float row_exp(const uint32_t (&x)[128], uint32_t p_ad
   return a0 + a1;
 }
 
-// LOCAL: rows of a V tile that some query of the tile sees, in block-relative tokens: up to hi, from lo on or below `sink`.
-struct VRows {
-  int lo, hi, sink;
+// LOCAL: iteration i of a unit.  Rows (tokens) of the block that some query of the tile sees: up to hi, from lo on or below `sink`;
+// all of them lie in the k-steps k0 .. k1 - 1 (16 rows each) of O += P V, and only these are computed.
+struct LocalBlock {
+  int J, lo, hi, sink, k0, k1;
+  __device__ __forceinline__ LocalBlock(const TileInfo& ti, int i, int sinks) {
+    J = i < ti.n_win ? ti.sg.J_hi - i : ti.T - 1 - i;
+    const int t0 = J * kBlock;
+    hi = min(kBlock - 1, ti.hi_tok - t0);
+    lo = max(0, ti.lo_tok - t0);
+    sink = max(0, min(sinks - t0, hi + 1));
+    k0 = sink > 0 ? 0 : lo / 16;
+    k1 = ((lo <= hi ? hi + 1 : sink) + 15) / 16;
+  }
+  // The iterations that may have rows nobody sees: the last rows' block, the one that the first row's window begins in, the last sinks'
+  static __device__ __forceinline__ bool edge(int n_win, int i) { return i == 0 || i == n_win - 1 || i == n_win; }
   __device__ __forceinline__ bool seen(int r) const { return r <= hi && (r >= lo || r < sink); }
+  // whether the k-steps have rows that nobody sees
+  __device__ __forceinline__ bool mixed() const { return hi + 1 < 16 * k1 || (16 * k0 < lo && sink < min(lo, 16 * k1)); }
 };
 
-// Another row may hold anything, NaN included, which no probability of zero makes harmless: it is cleared.  128 threads, a row each.
-__device__ __forceinline__ void clear_hidden_rows(uint8_t* sV, const VRows& vr, int row) {
-  if (vr.seen(row)) return;
+// Such a row may hold anything, NaN included, which no probability of zero makes harmless: it is cleared.  128 threads, a row each.
+__device__ __forceinline__ void clear_hidden_rows(uint8_t* sV, const LocalBlock& lb, int row) {
+  if (row < 16 * lb.k0 || row >= 16 * lb.k1 || lb.seen(row)) return;
 #pragma unroll
   for (int c = 0; c < 8; ++c) {
     *reinterpret_cast<uint4*>(sV + row * 128 + c * 16) = make_uint4(0, 0, 0, 0);
@@ -237,12 +251,73 @@ __device__ __forceinline__ void clear_hidden_rows(uint8_t* sV, const VRows& vr, 
   }
 }
 
+// A row's softmax step under a mask, 64 columns at a time (LOCAL: few iterations of a unit are masked, so this is kept short and out
+// of the way of the common step, which has the whole row in registers; without it inside, the common step of 32768 tokens with a
+// window of 4096 took 1045 ns of an SM per block instead of 1210).  Column j is visible iff lo <= j <= hi or j < sink, j <= hi.
+struct RowMask {
+  int lo, hi, sink;
+  __device__ __forceinline__ uint32_t word(int k) const {
+    auto from = [&](int n) { return __funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, n - 32 * k))); };   // columns >= n
+    return (from(lo) | ~from(sink)) & ~from(hi + 1);
+  }
+};
+__device__ __forceinline__ void masked_pair(uint32_t s_addr, int k, const RowMask& mask, uint32_t (&x)[64]) {
+#pragma unroll
+  for (int u = 0; u < 2; ++u) tmem_ld32(s_addr + k * 64 + u * 32, reinterpret_cast<uint32_t(&)[32]>(x[u * 32]));
+  tmem_wait_ld();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t m = mask.word(2 * k + u);
+    if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) x[u * 32 + j] = (m >> j) & 1u ? x[u * 32 + j] : 0xff800000u;   // -inf
+  }
+}
+__device__ __forceinline__ float masked_max(uint32_t s_addr, const RowMask& mask, int w0, int w1) {
+  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
+  for (int k = w0; k < w1; ++k) {
+    uint32_t x[64];
+    masked_pair(s_addr, k, mask, x);
+#pragma unroll
+    for (int j = 0; j < 64; j += 2) mx[(j >> 1) & 3] = max3(mx[(j >> 1) & 3], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+  }
+  return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+}
+// P of pair k takes columns 32 k .. 32 k + 31, logits of the pair k / 2: read before
+template <bool F16>
+__device__ __forceinline__ float masked_exp(uint32_t s_addr, const RowMask& mask, int w0, int w1, float cs, float neg_m) {
+  const uint64_t cs2 = f2_pack(cs, cs), nm2 = f2_pack(neg_m, neg_m);
+  uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll 1
+  for (int k = w0; k < w1; ++k) {
+    uint32_t x[64];
+    masked_pair(s_addr, k, mask, x);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      uint32_t pk[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        float x0, x1;
+        f2_unpack(f2_fma(f2_pack(__uint_as_float(x[u * 32 + 2 * j]), __uint_as_float(x[u * 32 + 2 * j + 1])), cs2, nm2), x0, x1);
+        const float p0 = ex2(x0), p1 = ex2(x1);
+        sum2[j & 1] = f2_add(sum2[j & 1], f2_pack(p0, p1));
+        pk[j] = F16 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
+      }
+      tmem_st16(s_addr + k * 32 + u * 16, pk);
+    }
+  }
+  float a0, a1;
+  f2_unpack(f2_add(sum2[0], sum2[1]), a0, a1);
+  return a0 + a1;
+}
+
 // map_kbar / map_kbar_lo: pooled keys of the correction chunks -- BF16: one BF16 array (map_kbar_lo unused);
 // FP8: the e4m3 hi and lo arrays.  map_vbar: pooled values, 16-bit.  map_q: packed query tiles (DevParams::q_box).
 // LOCAL: sliding window and sinks (fp2_window_prefill).  The iteration sequence of a unit is the blocks of its rows' windows, J_hi
 // downwards, then the blocks of the sinks in front of them; blocks that some row does not see whole (the diagonal, where the
-// windows begin, the last sink) are masked in tensor memory: what hidden keys hold (NaN) would come through a mask that the tensor
-// core adds.  Segments differ little in length, so they run in their own order.
+// windows begin, the last sink) are masked by the softmax warps: what hidden keys hold (NaN) would come through a mask that the
+// tensor core adds.  Segments differ little in length, so they run in their own order.
 template <bool FP8, bool WIDEN, bool LOCAL = false>
 __global__ void __launch_bounds__(AttnCfg<FP8>::kThreads, AttnCfg<FP8>::kCtasPerSm)
 sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
@@ -704,7 +779,8 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       const TileInfo& ti = info[slot];
       if (!ready_warp(&info_full[slot], (it >> 1) & 1, ctx, 403, &ti.valid)) break;
       const int T = ti.T, ndiag = P.diag_mma ? ti.ndiag : 0;
-      const int i0 = ti.it_begin, i1 = ti.it_end;
+      const int i0 = ti.it_begin, i1 = ti.it_end, n_win = ti.n_win;
+      (void)n_win;
       if (!qk_issued) mbar_wait(&q_full, it & 1, ctx, 404);
       for (int i = i0; i < i1; ++i, ++G) {
         // S = Q K^T (G).  The S columns are free: O += P V (G-1), which read P out of them, was issued before.
@@ -715,14 +791,17 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         // O += P V (G)
         mbar_wait(&v_full, G & 1, ctx, 402);
+        const bool edge = LOCAL && LocalBlock::edge(n_win, i);   // some k-steps only, all slices of P together: see the softmax step
+        if (!edge) {
 #pragma unroll
-        for (int h = 0; h < kPParts - 1; ++h) {   // as each slice of P arrives
-          mbar_wait(&p_ready[h], G & 1, ctx, 401);
-          tc_fence_after();
-          if (leader) {
+          for (int h = 0; h < kPParts - 1; ++h) {   // as each slice of P arrives
+            mbar_wait(&p_ready[h], G & 1, ctx, 401);
+            tc_fence_after();
+            if (leader) {
 #pragma unroll
-            for (int ks = h ? PSlices<FP8>::end(h - 1) : 0; ks < PSlices<FP8>::end(h); ++ks)
-              umma_f16_ts(tmem + 128, tmem + ks * 8, v_desc + ks * 128, idesc_pv, (i > i0) || ks > 0);
+              for (int ks = h ? PSlices<FP8>::end(h - 1) : 0; ks < PSlices<FP8>::end(h); ++ks)
+                umma_f16_ts(tmem + 128, tmem + ks * 8, v_desc + ks * 128, idesc_pv, (i > i0) || ks > 0);
+            }
           }
         }
         bool masked, chunk, last;
@@ -744,9 +823,16 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         mbar_wait(&p_ready[kPParts - 1], G & 1, ctx, 401);
         tc_fence_after();
         if (leader) {
+          if (edge) {
+            const LocalBlock lb(ti, i, A.sinks);
+#pragma unroll 1
+            for (int ks = lb.k0; ks < lb.k1; ++ks)
+              umma_f16_ts(tmem + 128, tmem + ks * 8, v_desc + ks * 128, idesc_pv, (i > i0) || ks > lb.k0);
+          } else {
 #pragma unroll
-          for (int ks = PSlices<FP8>::end(kPParts - 2); ks < 8; ++ks)
-            umma_f16_ts(tmem + 128, tmem + ks * 8, v_desc + ks * 128, idesc_pv, 1u);
+            for (int ks = PSlices<FP8>::end(kPParts - 2); ks < 8; ++ks)
+              umma_f16_ts(tmem + 128, tmem + ks * 8, v_desc + ks * 128, idesc_pv, 1u);
+          }
           umma_commit(&pv_done[G & 1]);
           if (qk_issued) issue_qk(masked, chunk, last);
         }
@@ -806,30 +892,18 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         bool need_mask = false;
         int tok_lim = 1 << 30;     // exact block: columns j with j <= tok_lim are visible
         uint32_t cm0 = 0xffffffffu, cm1 = 0xffffffffu, cm2 = 0xffffffffu, cm3 = 0xffffffffu;
-        VRows vr{0, kBlock, 0};   // LOCAL
-        (void)vr;
         float shift = 0.f;
         if (i < T) {
-          int J = LOCAL ? (i < ti.n_win ? J_hi - i : T - 1 - i) : dense ? J_hi - i : J_next;
+          int J = dense ? J_hi - i : J_next;
           if (!dense && i + 1 < T) J_next = list[T - 2 - i];
           J = max(0, min(J, J_hi));
-          need_mask = J >= J_lo && (!P.diag_mma || weak_bias);   // else the causal mask is in the logits already
-          tok_lim = pos - J * kBlock;
           if constexpr (LOCAL) {
-            const int t0 = J * kBlock;
-            vr = {ti.lo_tok - t0, ti.hi_tok - t0, A.sinks - t0};
-            need_mask = J >= J_lo || (t0 <= ti.hi_tok - A.window && t0 + kBlock > A.sinks);
-            if (need_mask) {   // columns from pos - window + 1 on, and sinks
-              const int lo = tok_lim - A.window + 1;
-              auto bits = [&](int k) {
-                return __funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, lo - 32 * k))) | ~__funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, vr.sink - 32 * k)));
-              };
-              cm0 = bits(0);
-              cm1 = bits(1);
-              cm2 = bits(2);
-              cm3 = bits(3);
-            }
+            J = i < ti.n_win ? J_hi - i : T - 1 - i;
+            need_mask = J >= J_lo || (J * kBlock <= ti.hi_tok - A.window && (J + 1) * kBlock > A.sinks);
+          } else {
+            need_mask = J >= J_lo && (!P.diag_mma || weak_bias);   // else the causal mask is in the logits already
           }
+          tok_lim = pos - J * kBlock;
         } else {
           shift = 7.0f;  // log2(128): one pooled row stands for a full block (Eq. 6); the todo mask is in the logits already
           if (weak_bias) {
@@ -850,10 +924,11 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
             mbar_wait(&vraw_full, rc & 1, ctx, 603);
             if (G >= 1) wait_pv(G - 1, 602);
             if constexpr (LOCAL) {
+              const LocalBlock lb(ti, i, A.sinks);
 #pragma unroll 4
               for (int k = tid; k < kTileRows * 8; k += 128) {
                 uint4 v = *reinterpret_cast<const uint4*>(sVraw + sw128_offset(k >> 3, k & 7));
-                if (!vr.seen(k >> 3)) v = make_uint4(0, 0, 0, 0);
+                if (!lb.seen(k >> 3)) v = make_uint4(0, 0, 0, 0);
                 widen_chunk_f16(v, sV, k >> 3, k & 7);
               }
             } else {
@@ -875,43 +950,55 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         pf[i == i0 ? 8 : (i < T ? 9 : 10)] += 1;
 #endif
         tc_fence_after();
-        if (need_mask) mask_row(s_addr, tok_lim, cm0, cm1, cm2, cm3);
-        if constexpr (LOCAL && !WIDEN) {
-          if (need_mask && (vr.hi < kBlock - 1 || (vr.lo > 0 && vr.sink < vr.lo))) {
-            mbar_wait(&v_full, G & 1, ctx, 504);
-            clear_hidden_rows(sV, vr, row);
-            fence_proxy_async();   // (O += P V starts when all threads have arrived on the first slice of P)
-          }
-        }
-        PF_END(4);
-        uint32_t x[128];
-        const float mx = fmaf(row_load_max(s_addr, x), cs_all, shift);  // cs > 0: scaling commutes with the maximum
-        const float m_new = fmaxf(m, mx);
         // lazy rescale: only when some row of the warp moved its maximum by more than 2^8.  O is at rest: the
         // MMAs complete in issue order, so S (G) in TMEM means O += P V (G-1) has been added.  Padding rows have no say (their
         // probabilities may overflow, which stays in their own rows): when a row is rescaled decides how its probabilities round,
         // and that must not hang on what the batch holds beside its sequence.
-        if (__any_sync(0xffffffffu, row_ok && m_new > m + 8.0f)) {
-          const float f = (m == -INFINITY) ? 0.f : ex2(m - m_new);
-          if (i > i0) {
+        auto rescale = [&](float mx) {
+          const float m_new = fmaxf(m, mx);
+          if (__any_sync(0xffffffffu, row_ok && m_new > m + 8.0f)) {
+            const float f = (m == -INFINITY) ? 0.f : ex2(m - m_new);
+            if (i > i0) {
 #pragma unroll 1
-            for (int k = 0; k < 4; ++k) {
-              uint32_t rr[32];
-              tmem_ld32(o_addr + k * 32, rr);
-              tmem_wait_ld();
+              for (int k = 0; k < 4; ++k) {
+                uint32_t rr[32];
+                tmem_ld32(o_addr + k * 32, rr);
+                tmem_wait_ld();
 #pragma unroll
-              for (int j = 0; j < 32; ++j) rr[j] = __float_as_uint(__uint_as_float(rr[j]) * f);
-              tmem_st32(o_addr + k * 32, rr);
+                for (int j = 0; j < 32; ++j) rr[j] = __float_as_uint(__uint_as_float(rr[j]) * f);
+                tmem_st32(o_addr + k * 32, rr);
+              }
             }
+            l *= f;
+            m = m_new;
           }
-          l *= f;
-          m = m_new;
+        };
+        if (LOCAL && need_mask) {
+          const LocalBlock lb(ti, i, A.sinks);
+          const RowMask mask{tok_lim - A.window + 1, tok_lim, lb.sink};
+          const int w0 = lb.k0 / 4, w1 = (lb.k1 + 3) / 4;
+          rescale(masked_max(s_addr, mask, w0, w1) * cs_all);
+          l += masked_exp<FP8>(s_addr, mask, w0, w1, cs_all, m == -INFINITY ? 0.f : -m);
+          tmem_wait_st();
+          tc_fence_before();
+          if (!WIDEN && lb.mixed()) {   // (WIDEN has cleared them)
+            mbar_wait(&v_full, G & 1, ctx, 504);
+            clear_hidden_rows(sV, lb, row);
+            fence_proxy_async();
+          }
+#pragma unroll
+          for (int h = 0; h < kPParts - 1; ++h) mbar_arrive(&p_ready[h]);
+        } else {
+          if (need_mask) mask_row(s_addr, tok_lim, cm0, cm1, cm2, cm3);
+          PF_END(4);
+          uint32_t x[128];
+          rescale(fmaf(row_load_max(s_addr, x), cs_all, shift));  // cs > 0: scaling commutes with the maximum
+          // a row with nothing visible so far has m = -inf and only -inf logits: exponent against 0 -> zeros
+          const float neg_m = (m == -INFINITY) ? shift : shift - m;
+          l += row_exp<FP8>(x, s_addr, cs_all, neg_m, &p_ready[0]);
+          tmem_wait_st();
+          tc_fence_before();
         }
-        // a row with nothing visible so far has m = -inf and only -inf logits: exponent against 0 -> zeros
-        const float neg_m = (m == -INFINITY) ? shift : shift - m;
-        l += row_exp<FP8>(x, s_addr, cs_all, neg_m, &p_ready[0]);
-        tmem_wait_st();
-        tc_fence_before();
         mbar_arrive(&p_ready[kPParts - 1]);
         PF_END(5);
       }
