@@ -396,9 +396,31 @@ decode_kernel(DecodeArgs A) {
     cp_async_commit();
   };
 
+  // Queries: lane (l4, c) holds row l4 of each 8-row tile, and of the contraction the dims that its 16-byte pieces of K hold: step s,
+  // dims 32 c + 4 s .. + 3 (e4m3) or 64 (s >> 2) + 16 c + 4 (s & 3) .. + 3 (BF16).  Asked for ahead of the unit's copies: behind
+  // them, with the memory busy, they took 4000 cycles.
+  uint4 qraw[NR][4];
+  float k_scale = 1.f, v_scale = 1.f;
+  auto load_q = [&](const DecodeUnit& u) {
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      int tok, head;
+      row_of(u, min(n * 8 + l4, u.nrows - 1), tok, head);
+      const uint8_t* src = A.q + (long long)(u.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2);
+#pragma unroll
+      for (int s = 0; s < 4; ++s)
+        qraw[n][s] = *reinterpret_cast<const uint4*>(src + 2 * (FP8 ? 32 * c + 8 * s : 64 * (s >> 1) + 16 * c + 8 * (s & 1)));
+    }
+    if constexpr (FMT == FMT_FP8_HEAD) {
+      k_scale = A.k_scale[u.h];
+      v_scale = A.v_scale[u.h];
+    }
+  };
+
   DecodeUnit u;
   if (!next_unit(u)) return;
   pids_next = load_pids(u, u.i0);
+  load_q(u);
 #pragma unroll 1
   for (int k = 0; k < Cfg::kEarly; ++k) issue(u, k, k);
   for (;;) {
@@ -406,8 +428,6 @@ decode_kernel(DecodeArgs A) {
     for (int k = Cfg::kEarly; k < ST - 1; ++k) issue(u, k, k);
 
     // ------------------------------ queries ------------------------------
-    // Lane (l4, c) holds row l4 of each 8-row tile, and of the contraction the dims that its 16-byte pieces of K hold: step s,
-    // dims 32 c + 4 s .. + 3 (e4m3) or 64 (s >> 2) + 16 c + 4 (s & 3) .. + 3 (BF16).
     uint32_t qb[NR][8][2];
     float cs[NR][2];                     // multipliers of rows 2 c, 2 c + 1: what a lane's logits belong to
     int prow[NR][2];
@@ -415,14 +435,12 @@ decode_kernel(DecodeArgs A) {
     for (int n = 0; n < NR; ++n) {
       int tok, head;
       row_of(u, min(n * 8 + l4, u.nrows - 1), tok, head);
-      const uint8_t* src = A.q + (long long)(u.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2);
 #pragma unroll
-      for (int s = 0; s < 8; s += 2) {
-        const uint4 x = *reinterpret_cast<const uint4*>(src + 2 * (FP8 ? 32 * c + 4 * s : 64 * (s >> 2) + 16 * c + 4 * (s & 3)));
-        qb[n][s][0] = x.x;
-        qb[n][s][1] = x.y;
-        qb[n][s + 1][0] = x.z;
-        qb[n][s + 1][1] = x.w;
+      for (int s = 0; s < 4; ++s) {
+        qb[n][2 * s][0] = qraw[n][s].x;
+        qb[n][2 * s][1] = qraw[n][s].y;
+        qb[n][2 * s + 1][0] = qraw[n][s].z;
+        qb[n][2 * s + 1][1] = qraw[n][s].w;
       }
       float mul = A.scale_log2;
       if constexpr (FP8) {
@@ -438,7 +456,7 @@ decode_kernel(DecodeArgs A) {
         e = a == 0 || a >= 0x7f80u ? 0 : max(-126, min(126, e));
         const float f = __uint_as_float((uint32_t)(e + 127) << 23), back = __uint_as_float((uint32_t)(127 - e) << 23);
         mul *= back;
-        if constexpr (FMT == FMT_FP8_HEAD) mul *= A.k_scale[u.h];
+        if constexpr (FMT == FMT_FP8_HEAD) mul *= k_scale;
         mul = fmaxf(mul, 1e-37f);        // (a hidden logit of -inf times zero would be NaN)
 #pragma unroll
         for (int s = 0; s < 8; ++s)
@@ -454,14 +472,7 @@ decode_kernel(DecodeArgs A) {
     DecodeUnit un;                       // the next one: known early, so that its page ids are there when this one ends
     const bool more = next_unit(un);
     const int pids_un = more ? load_pids(un, un.i0) : -1;
-    if (more && warp == 0) {             // and its queries
-#pragma unroll
-      for (int k = lane; k < 2 * RT; k += 32) {
-        int tok, head;
-        row_of(un, k >> 1, tok, head);
-        if (k >> 1 < un.nrows) prefetch_l1(A.q + (long long)(un.c0 + tok) * A.q_stride_bytes + head * (kHeadDim * 2) + (k & 1) * 128);
-      }
-    }
+    const float out_scale = FMT == FMT_FP8_HEAD ? v_scale : 1.f;
 
     float o[NR][8][4];                   // tile t: rows 2 c, 2 c + 1 of two dims of this lane's
     float m[NR][2], l[NR][2];
@@ -649,6 +660,7 @@ decode_kernel(DecodeArgs A) {
     // waited for in its last step.)
     __syncwarp();
     if (more) {
+      if constexpr (NR <= 2) load_q(un);
       pids_next = pids_un;
 #pragma unroll 1
       for (int k = 0; k < Cfg::kEarly; ++k) issue(un, k, k);
@@ -674,7 +686,8 @@ decode_kernel(DecodeArgs A) {
           *reinterpret_cast<float4*>(orow + piece(row, dim >> 2) * 4) = make_float4(o[n][t][v], o[n][t][2 + v], o[n][t + 1][v], o[n][t + 1][2 + v]);
         }
       }
-    const float out_scale = FMT == FMT_FP8_HEAD ? A.v_scale[u.h] : 1.f;
+    if constexpr (NR > 2)                // (where O leaves no registers for them)
+      if (more) load_q(un);
     // Joins what the warps have put into shared memory.  place < 0: to out and lse; else to that row of the partial results.
     auto join = [&](long long place) {
       __syncthreads();
