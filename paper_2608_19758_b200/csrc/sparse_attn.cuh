@@ -62,9 +62,13 @@ struct TileInfo {
   int32_t it_begin, it_end;   // this unit's part of the iteration sequence [0, T + nchunk) (Eq. 18); all of it unless split
   int32_t parts;              // parts the segment is split into (1: the unit writes the final output)
   int32_t slot;               // partial-result slot of this unit when parts > 1
-  int32_t n_win;              // LOCAL: iterations of the window; those of the sinks follow
-  int32_t lo_tok, hi_tok;     // LOCAL: first token of the first row's window, position of the last row
-  int32_t chunk_id[kMaxChunks];
+  union {
+    int32_t chunk_id[kMaxChunks];
+    struct {                  // LOCAL (which has no correction chunks)
+      int32_t n_win;          // iterations of the window; those of the sinks follow
+      int32_t lo_tok, hi_tok; // first token of the first row's window, position of the last row
+    };
+  };
   uint32_t todo[kMaxChunks][4];
 };
 
