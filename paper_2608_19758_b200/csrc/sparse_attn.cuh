@@ -440,10 +440,10 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       if constexpr (!FP8)
         tma_load_3d_hint(dst + AttnCfg<FP8>::kQHalf, &map_q, &q_full, 64, sg.h * g, sg.q_tok0 + tok0, pol);
     };
-    if (t64 < 32)
+    if (!LOCAL && t64 < 32)
       for (int w = t64; w < kMaxBlocks / 32; w += 32) sel_bits[w] = 0u;
     if (t64 == 0) ndiag_s = 0;
-    const int n_units = A.unit_split ? *A.n_units : P.nseg;
+    const int n_units = !LOCAL && A.unit_split ? *A.n_units : P.nseg;
     // Both warps run through the same named barriers whatever a wait gives: they leave by unit_s alone, which one thread sets.
     for (int it = 0;; ++it) {
       const int slot = it & 1;
@@ -474,7 +474,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         n_win = sg.J_hi - lo_tok / kBlock + 1;
         T = n_win + min((A.sinks + kBlock - 1) / kBlock, lo_tok / kBlock);
       }
-      if (T < 0 || T > sg.J_hi + 1) {  // malformed count: clamp so every loop stays bounded
+      if (!LOCAL && (T < 0 || T > sg.J_hi + 1)) {  // malformed count: clamp so every loop stays bounded
         if (t64 == 0) atomicOr(A.status + ST_BAD_LIST, 1);
         T = max(0, min(T, sg.J_hi + 1));
       }
@@ -521,7 +521,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           nchunk = __popc(bal);
         }
         if (t64 == 0) {
-          const int32_t split = A.unit_split ? A.unit_split[w] : pack_split(0, 1, 0);
+          const int32_t split = !LOCAL && A.unit_split ? A.unit_split[w] : pack_split(0, 1, 0);
           const int parts = (split >> 8) & 0xff, u = split & 0xff, n = T + nchunk;
           ti.sg = sg;
           ti.valid = 1;
@@ -550,7 +550,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const bool free = mbar_wait(&q_empty, (it - 1) & 1, ctx, 202);
         if (P.q_box && t64 == 0 && free) issue_q(sg);
       }
-      {   // sHot: rows 2 t64 and 2 t64 + 1
+      if constexpr (!LOCAL) {   // sHot: rows 2 t64 and 2 t64 + 1
         const int rem = sg.r0 % g;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -641,7 +641,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         const int pid = pid_next;
         const int J_cur = J_fetched;
         if (G >= 1) live &= mbar_wait(&s_done, (G - 1) & 1, ctx, 302);   // K stage free
-        if (i < T) {
+        if (LOCAL || i < T) {
           const int nvalid = __popc(__ballot_sync(0xffffffffu, pid >= 0));
           const uint32_t bytes = (uint32_t)nvalid * psz * (FP8 ? 128u : 256u);
           request_k(bytes, [&]() {
@@ -651,7 +651,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
               if constexpr (!FP8) tma_load_3d_hint(sK + 16384 + lane * psz * 128, &map_k, &k_full, 64, sg.h, pid * psz, keep);
             }
           }, [&]() {
-            if (i < ti.ndiag && P.diag_mma) {
+            if (!LOCAL && i < ti.ndiag && P.diag_mma) {
               // diagonal block: column j is hidden from the tile's position c iff J * 128 + j > pre + r0 / g + c
               const int t0 = sg.pre + sg.r0 / g - J_cur * kBlock;
 #pragma unroll 1
@@ -791,7 +791,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (!qk_issued) {
           mbar_wait(&k_full, G & 1, ctx, 405);
           tc_fence_after();
-          if (leader) issue_qk(i >= T || i < ndiag, i >= T, i == i1 - 1);
+          if (leader) issue_qk(!LOCAL && (i >= T || i < ndiag), !LOCAL && i >= T, i == i1 - 1);
         }
         // O += P V (G)
         mbar_wait(&v_full, G & 1, ctx, 402);
@@ -810,8 +810,8 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         }
         bool masked, chunk, last;
         if (i + 1 < i1) {
-          masked = i + 1 >= T || i + 1 < ndiag;
-          chunk = i + 1 >= T;
+          masked = !LOCAL && (i + 1 >= T || i + 1 < ndiag);
+          chunk = !LOCAL && i + 1 >= T;
           last = i + 1 == i1 - 1;
           qk_issued = mbar_test(&k_full, (G + 1) & 1);
         } else {
@@ -819,8 +819,8 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           qk_issued = mbar_test(&info_full[slot ^ 1], ((it + 1) >> 1) & 1);
           if (qk_issued)
             qk_issued = tn.valid && tn.it_begin < tn.it_end && mbar_test(&q_full, (it + 1) & 1) && mbar_test(&k_full, (G + 1) & 1);
-          masked = qk_issued && (tn.it_begin >= tn.T || (P.diag_mma && tn.it_begin < tn.ndiag));
-          chunk = qk_issued && tn.it_begin >= tn.T;
+          masked = !LOCAL && qk_issued && (tn.it_begin >= tn.T || (P.diag_mma && tn.it_begin < tn.ndiag));
+          chunk = !LOCAL && qk_issued && tn.it_begin >= tn.T;
           last = qk_issued && tn.it_begin == tn.it_end - 1;
         }
         qk_issued = __all_sync(0xffffffffu, qk_issued);
@@ -843,7 +843,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       }
       __syncwarp();   // no lane reads the descriptor any more
       if (leader) {
-        if (i1 == i0) umma_commit(&q_empty);  // nothing to do for this unit: nothing read Q, release it at once
+        if (!LOCAL && i1 == i0) umma_commit(&q_empty);  // nothing to do for this unit: nothing read Q, release it at once
         mbar_arrive(&info_empty[slot]);
       }
     }
@@ -870,7 +870,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       if (!ready_warp(&info_full[slot], (it >> 1) & 1, ctx, 501, &ti.valid)) break;
       PF_END(0);
       const int T = ti.T;
-      const bool dense = ti.dense != 0;
+      const bool dense = LOCAL || ti.dense != 0;
       const int J_hi = ti.sg.J_hi, J_lo = ti.sg.J_lo;
       const int32_t* list = A.blk_idx + ti.sg.off;
       const int r = ti.sg.r0 + row;
@@ -885,7 +885,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       // The mask bias is -3.3e9 in raw units; with FP8 scales so small that this is no longer far below every
       // visible logit of the row, the warp masks in TMEM as well.
       bool weak_bias = false;
-      if constexpr (FP8) weak_bias = __any_sync(0xffffffffu, !(cs_all * 3.0e9f > 256.f));
+      if constexpr (FP8) weak_bias = !LOCAL && __any_sync(0xffffffffu, !(cs_all * 3.0e9f > 256.f));
       const bool row_ok = row < ti.sg.nrows;   // else padding: whatever queries follow, those of other sequences among them
       float m = -INFINITY, l = 0.f;
       // block id of the next exact iteration, fetched one iteration ahead
@@ -897,7 +897,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         int tok_lim = 1 << 30;     // exact block: columns j with j <= tok_lim are visible
         uint32_t cm0 = 0xffffffffu, cm1 = 0xffffffffu, cm2 = 0xffffffffu, cm3 = 0xffffffffu;
         float shift = 0.f;
-        if (i < T) {
+        if (LOCAL || i < T) {
           int J = dense ? J_hi - i : J_next;
           if (!dense && i + 1 < T) J_next = list[T - 2 - i];
           J = max(0, min(J, J_hi));
@@ -924,7 +924,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
           // at the logits.  128 threads take ~900 cycles (the copy is bound by shared-memory bandwidth next to the
           // other CTA's MMAs); one or two dedicated warps were slower than the time they have, between
           // O += P V (G-1) freeing the stage and the first slice of P (G) needing it.
-          if (i < T) {
+          if (LOCAL || i < T) {
             mbar_wait(&vraw_full, rc & 1, ctx, 603);
             if (G >= 1) wait_pv(G - 1, 602);
             if constexpr (LOCAL) {
@@ -993,7 +993,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
 #pragma unroll
           for (int h = 0; h < kPParts - 1; ++h) mbar_arrive(&p_ready[h]);
         } else {
-          if (need_mask) mask_row(s_addr, tok_lim, cm0, cm1, cm2, cm3);
+          if (!LOCAL && need_mask) mask_row(s_addr, tok_lim, cm0, cm1, cm2, cm3);
           PF_END(4);
           uint32_t x[128];
           rescale(fmaf(row_load_max(s_addr, x), cs_all, shift));  // cs > 0: scaling commutes with the maximum
@@ -1010,7 +1010,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
       PF_BEGIN();
       const SegInfo& sg = ti.sg;
       const float inv = l > 0.f ? out_scale / l : 0.f;
-      const bool have_o = i1 > i0;
+      const bool have_o = LOCAL || i1 > i0;
       const size_t tok = (size_t)sg.q_tok0 + r / g;
       const int head = sg.h * g + r % g;
       __nv_bfloat16* orow = A.out + (tok * P.num_q_heads + head) * kHeadDim;
@@ -1019,7 +1019,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         tc_fence_after();
       }
       PF_END(6);
-      if (ti.parts > 1) {
+      if (!LOCAL && ti.parts > 1) {
         // one part of a split segment (Eq. 18): leave (O, m, l) unnormalised for the merge kernel
         float* prow = A.part_o + ((size_t)ti.slot * 128 + row) * 128;
         if (have_o) {
