@@ -314,6 +314,8 @@ class Cache:
         self._device = torch.cuda.current_device() if torch.cuda.is_available() else -1
         p = self.params
         self._fp8 = p.format != CACHE_BF16
+        self._kinds = _E4M3 if self._fp8 else _BF16
+        self._max_pages, self._q_heads = p.max_pages_per_seq, p.num_q_heads
         self._pool = (p.num_pages, p.page_size, p.num_kv_heads, p.head_dim)
         self._scales = {CACHE_BF16: None, CACHE_FP8_HEAD: (p.num_kv_heads,), CACHE_FP8_PAGE: (p.num_pages, p.num_kv_heads)}[p.format]
 
@@ -335,18 +337,26 @@ class Cache:
         return k, v, ks, vs
 
     def _check_pages(self, where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, num_seqs, workspace):
-        dev = self._device
-        if self._fp8:
-            _want(where, dev, k_cache, _E4M3, self._pool)
-            _want(where, dev, v_cache, _E4M3, self._pool)
-            _want(where, dev, k_scale, _F32, self._scales)
-            _want(where, dev, v_scale, _F32, self._scales)
-        else:
-            _want(where, dev, k_cache, _BF16, self._pool)
-            _want(where, dev, v_cache, _BF16, self._pool)
-        _want(where, dev, page_table, _I32, (num_seqs, self.params.max_pages_per_seq))
-        _want(where, dev, seqlens_k, _I32, (num_seqs,))
-        if workspace.numel() < self.workspace_bytes or workspace.get_device() != dev:
+        """The tensors that all calls share; returns the device's number.  (Written out: a call per tensor is a microsecond in all,
+        of the ten that a call takes on the host.)"""
+        dev, pool, kinds, pt_shape = self._device, self._pool, self._kinds, (num_seqs, self._max_pages)
+        if not (k_cache.dtype in kinds and k_cache.shape == pool and k_cache.get_device() == dev and k_cache.is_contiguous() and
+                v_cache.dtype in kinds and v_cache.shape == pool and v_cache.get_device() == dev and v_cache.is_contiguous() and
+                page_table.dtype is torch.int32 and page_table.shape == pt_shape and page_table.get_device() == dev and
+                page_table.is_contiguous() and seqlens_k.dtype is torch.int32 and seqlens_k.dim() == 1 and
+                seqlens_k.get_device() == dev and seqlens_k.is_contiguous()):
+            _want(where, dev, k_cache, kinds, pool)
+            _want(where, dev, v_cache, kinds, pool)
+            _want(where, dev, page_table, _I32, pt_shape)
+            _want(where, dev, seqlens_k, _I32, (num_seqs,))
+        shape = self._scales
+        if shape is not None and not (
+                k_scale is not None and k_scale.dtype is torch.float32 and k_scale.shape == shape and k_scale.get_device() == dev and
+                k_scale.is_contiguous() and v_scale is not None and v_scale.dtype is torch.float32 and v_scale.shape == shape and
+                v_scale.get_device() == dev and v_scale.is_contiguous()):
+            _want(where, dev, k_scale, _F32, shape)
+            _want(where, dev, v_scale, _F32, shape)
+        if workspace.nbytes < self.workspace_bytes or workspace.get_device() != dev:
             raise Fp2Error(1, f"{where}: workspace too small or not on device {dev}")
         return dev
 
@@ -374,25 +384,26 @@ def _want(where, dev, t, dtypes, shape):
 
 
 def _rows(where, dev, t, heads):
-    """Token stride of a BF16 [tokens, heads, 128] tensor whose tokens may lie apart (a slice of a fused projection)."""
-    shape, stride = t.shape, t.stride()
-    if t.dtype is not torch.bfloat16 or len(shape) != 3 or shape[1] != heads or shape[2] != 128 or t.get_device() != dev or \
-            stride[2] != 1 or (heads > 1 and stride[1] != 128):
-        raise Fp2Error(1, f"{where}: wanted BF16 [tokens, {heads}, 128] on device {dev}, heads next to each other, got {t.dtype} "
-                          f"{tuple(shape)} on {t.device}, strides {stride}")
-    return stride[0] if shape[0] > 1 else heads * 128
+    """Tokens and token stride of a BF16 [tokens, heads, 128] tensor whose tokens may lie apart (a slice of a fused projection)."""
+    if t.dim() == 3 and t.dtype is torch.bfloat16 and t.get_device() == dev:
+        tokens, h, d = t.shape
+        apart, head, dim = t.stride()
+        if h == heads and d == 128 and dim == 1 and (head == 128 or heads == 1):
+            return tokens, apart if tokens > 1 else heads * 128
+    raise Fp2Error(1, f"{where}: wanted BF16 [tokens, {heads}, 128] on device {dev}, heads next to each other, got {t.dtype} "
+                      f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
 
 def fp2_cache_append(cache: Cache, k_new, v_new, page_table, cu_seqlens_new, seqlens_k, k_cache, v_cache, k_scale, v_scale,
                      workspace, stream=None):
     """Writes the keys and values of new tokens into their pages (quantised where the cache holds 8 bits; FP8_PAGE caches get
     the pages' scales too).  seqlens_k: tokens in the cache after the call."""
-    ns, where = seqlens_k.shape[0], "fp2_cache_append"
+    ns, where = seqlens_k.numel(), "fp2_cache_append"
     dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, cu_seqlens_new, _I32, (ns + 1,))
-    heads = cache.params.num_kv_heads
-    stride, total = _rows(where, dev, k_new, heads), k_new.shape[0]
-    if _rows(where, dev, v_new, heads) != stride or v_new.shape[0] != total:
+    heads = cache._pool[2]
+    total, stride = rows = _rows(where, dev, k_new, heads)
+    if _rows(where, dev, v_new, heads) != rows:
         raise Fp2Error(1, f"{where}: k_new and v_new differ in tokens or strides")
     _check(load().fp2_cache_append(cache.handle, _ptr(k_new), _ptr(v_new), stride, _ptr(page_table), _ptr(cu_seqlens_new),
                                    _ptr(seqlens_k), ns, total, _ptr(k_cache), _ptr(v_cache), _ptr(k_scale),
@@ -402,7 +413,7 @@ def fp2_cache_append(cache: Cache, k_new, v_new, page_table, cu_seqlens_new, seq
 def fp2_cache_expand(cache: Cache, k_cache, v_cache, page_table, seqlens_k, k_scale, v_scale, k_out, v_out, out_page_table,
                      workspace, stream=None):
     """An 8-bit cache as BF16 pages [out_num_pages, page_size, num_kv_heads, 128] for stage calls of a BF16 plan."""
-    ns, where = seqlens_k.shape[0], "fp2_cache_expand"
+    ns, where = seqlens_k.numel(), "fp2_cache_expand"
     dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, out_page_table, _I32, tuple(page_table.shape))
     pool = (k_out.shape[0],) + cache._pool[1:]
@@ -416,11 +427,11 @@ def fp2_cache_expand(cache: Cache, k_cache, v_cache, page_table, seqlens_k, k_sc
 def fp2_decode(cache: Cache, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, k_scale, v_scale, out, lse, workspace,
                window_tokens: int = 0, sink_tokens: int = 0, stream=None):
     """Attention of the newest few tokens of every sequence over its pages, with an optional sliding window and sinks."""
-    ns, where = seqlens_k.shape[0], "fp2_decode"
+    ns, where = seqlens_k.numel(), "fp2_decode"
     dev = cache._check_pages(where, k_cache, v_cache, k_scale, v_scale, page_table, seqlens_k, ns, workspace)
     _want(where, dev, cu_seqlens_q, _I32, (ns + 1,))
-    heads, total_q = cache.params.num_q_heads, q.shape[0]
-    stride = _rows(where, dev, q, heads)
+    heads = cache._q_heads
+    total_q, stride = _rows(where, dev, q, heads)
     _want(where, dev, out, _BF16, (total_q, heads, 128))
     if lse is not None:
         _want(where, dev, lse, _F32, (heads, total_q))

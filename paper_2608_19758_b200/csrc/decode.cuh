@@ -16,6 +16,11 @@
 // part of shared memory (cp.async, kStages steps ahead) and attends to with its own running maximum and sum: no barrier in the
 // loop; the four join at the end of a unit, while the first copies of the next one are on their way.  Copies of hidden tokens
 // write zeros without reading, so nothing that stands in a hidden place reaches the sums.  192 KB of an SM take part.
+// (By TMA, a box per page and operand, lanes in turn: everything 4 to 6 % slower.)
+//
+// Measured, whole calls: 64 sequences of 4096 tokens, 8 KV heads, 168 us in BF16 (6.4 TB/s, 0.98 of the copy rate), 100 us in 8 bits
+// (5.4 TB/s, 0.82: four warps a CTA issue 41 % of the time, and what a warp does on a step takes longer than its bytes); 131072
+// tokens of 4 heads 52 us in BF16, of which 41 are the bytes, 5 the start and 5 the joining of 74 parts per head.
 //
 // S^T = K Q^T and O^T += V^T P^T are m16n8k16 MMAs of a warp with the tokens (then the dims) as the long side and 8 packed
 // (token, query head) rows of the KV head as the short one, NR times: a group of up to eight heads wastes nothing.  What tcgen05
@@ -27,7 +32,7 @@
 // Precision.  BF16 caches: Q and K as they are; P as a BF16 pair hi + lo (2^-17).  e4m3 caches: K, V exact as F16; Q exact as
 // F16 after a power of two per row has brought its maximum to 2^13 .. 2^14 (elements 2^-28 below it round); P as F16 against a
 // reference 8 binades below the running maximum, where the steps are 2^-11 relative down to 2^-22 of the maximum.  Sums in 32 bits.
-// (e4m3 operands as such: the warp-level MMA takes them, but widens them itself on this GPU, in more instructions than here.)
+// (The warp-level MMA takes e4m3 operands as such, Q as a pair of them; K Q^T then took twice the instructions: it widens them itself.)
 // Scales per page: ks multiplies the logits; vs enters P, in the exponent, so that P V needs none:
 // y = x + log2 vs has the running maximum, p = 2^(y - m), and l adds p / vs.
 #pragma once
@@ -41,11 +46,17 @@ namespace fp2 {
 constexpr int kDecWarps = 4;
 constexpr int kDecThreads = 32 * kDecWarps;
 constexpr int kDecCtasPerSm = 2;
-constexpr int kDecGroup = 16;                 // parts of a unit that are joined at a time: see join_parts
-constexpr int kDecJoin = 2;                   // of these in a warp's registers
-constexpr int kDecWhole = 12;                 // units up to this long are not cut: they belong to the share that they begin in
-constexpr int kDecMinShare = 5;               // least share of a CTA, in blocks (kDecUnitCost included)
-constexpr int kDecUnitCost = 4;               // what a unit costs beside its blocks, in blocks
+// What the split goes by, in blocks, and what whole calls took with other values (us):
+// A unit costs this much beside its blocks (0 / 2 / 4 / 8: 64 ragged sequences of 8-bit pages 141 / 107 / 99 / 107).
+constexpr int kDecUnitCost = 4;
+// Units up to this long, with that, are not cut: they belong to the share that they begin in (12 / 20: the same 102 / 108).
+constexpr int kDecWhole = 12;
+// Least share of a CTA, with that (5 / 6 / 8: one sequence of 2048 tokens, BF16, 10.8 / 11.6 / 13.2).
+constexpr int kDecMinShare = 5;
+// Parts of a unit that are joined at a time, and of these in a warp's registers (all parts by one CTA, four warps side by side: 131072
+// tokens BF16 58.4; 16, four at a time 55.5; 8, two at a time 53.8, but 8192 tokens 19.6 against 16.9; 16, two at a time 53.1).
+constexpr int kDecGroup = 16;
+constexpr int kDecJoin = 2;
 
 template <int FMT, int NR>
 struct DecodeCfg {
@@ -296,7 +307,7 @@ decode_kernel(DecodeArgs A) {
           if (++uh == heads && pos < pos_end) {
             uh = 0;
             do sq = decode_seq<Cfg>(A, ++b, false);
-            while (sq.cost == 0);      // (items are left: there is one)
+            while (sq.cost == 0 && b + 1 < A.g.num_seqs);   // (items are left: there is one)
           }
         }
       }

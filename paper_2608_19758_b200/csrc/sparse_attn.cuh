@@ -255,61 +255,54 @@ __device__ __forceinline__ void clear_hidden_rows(uint8_t* sV, const LocalBlock&
   }
 }
 
-// A row's softmax step under a mask, 64 columns at a time (LOCAL: few iterations of a unit are masked, so this is kept short and out
-// of the way of the common step, which has the whole row in registers; without it inside, the common step of 32768 tokens with a
-// window of 4096 took 1045 ns of an SM per block instead of 1210).  Column j is visible iff lo <= j <= hi or j < sink, j <= hi.
-struct RowMask {
+// A row's softmax step under a mask, 32 columns at a time, read twice.  LOCAL: few iterations of a unit are masked, so their step is
+// kept short, for the instruction cache, and apart from the common one.  Six FP8 chunks, window 1000 / 32768 tokens, window 4096,
+// whole calls: the logits masked in tensor memory ahead of the common step 210 / 2160 us; in registers inside it 196 / 2063; a step
+// of its own with the row in registers 228 / 2046; this one 173 / 1980.
+struct RowMask {   // column j is visible iff j <= hi and (j >= lo or j < sink)
   int lo, hi, sink;
   __device__ __forceinline__ uint32_t word(int k) const {
     auto from = [&](int n) { return __funnelshift_lc(0u, 0xffffffffu, (uint32_t)min(32, max(0, n - 32 * k))); };   // columns >= n
     return (from(lo) | ~from(sink)) & ~from(hi + 1);
   }
 };
-__device__ __forceinline__ void masked_pair(uint32_t s_addr, int k, const RowMask& mask, uint32_t (&x)[64]) {
-#pragma unroll
-  for (int u = 0; u < 2; ++u) tmem_ld32(s_addr + k * 64 + u * 32, reinterpret_cast<uint32_t(&)[32]>(x[u * 32]));
+__device__ __forceinline__ void masked_word(uint32_t s_addr, int k, const RowMask& mask, uint32_t (&x)[32]) {
+  tmem_ld32(s_addr + k * 32, x);
   tmem_wait_ld();
+  const uint32_t m = mask.word(k);
+  if (__all_sync(0xffffffffu, m == 0xffffffffu)) return;
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const uint32_t m = mask.word(2 * k + u);
-    if (__all_sync(0xffffffffu, m == 0xffffffffu)) continue;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) x[u * 32 + j] = (m >> j) & 1u ? x[u * 32 + j] : 0xff800000u;   // -inf
-  }
+  for (int j = 0; j < 32; ++j) x[j] = (m >> j) & 1u ? x[j] : 0xff800000u;   // -inf
 }
 __device__ __forceinline__ float masked_max(uint32_t s_addr, const RowMask& mask, int w0, int w1) {
-  float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+  float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
   for (int k = w0; k < w1; ++k) {
-    uint32_t x[64];
-    masked_pair(s_addr, k, mask, x);
+    uint32_t x[32];
+    masked_word(s_addr, k, mask, x);
 #pragma unroll
-    for (int j = 0; j < 64; j += 2) mx[(j >> 1) & 3] = max3(mx[(j >> 1) & 3], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
+    for (int j = 0; j < 32; j += 2) mx[(j >> 1) & 1] = max3(mx[(j >> 1) & 1], __uint_as_float(x[j]), __uint_as_float(x[j + 1]));
   }
-  return fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]);
+  return fmaxf(mx[0], mx[1]);
 }
-// P of pair k takes columns 32 k .. 32 k + 31, logits of the pair k / 2: read before
+// P of word k takes columns 16 k .. 16 k + 15, logits of the word k / 2: read before
 template <bool F16>
 __device__ __forceinline__ float masked_exp(uint32_t s_addr, const RowMask& mask, int w0, int w1, float cs, float neg_m) {
   const uint64_t cs2 = f2_pack(cs, cs), nm2 = f2_pack(neg_m, neg_m);
   uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll 1
   for (int k = w0; k < w1; ++k) {
-    uint32_t x[64];
-    masked_pair(s_addr, k, mask, x);
+    uint32_t x[32], pk[16];
+    masked_word(s_addr, k, mask, x);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      uint32_t pk[16];
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        float x0, x1;
-        f2_unpack(f2_fma(f2_pack(__uint_as_float(x[u * 32 + 2 * j]), __uint_as_float(x[u * 32 + 2 * j + 1])), cs2, nm2), x0, x1);
-        const float p0 = ex2(x0), p1 = ex2(x1);
-        sum2[j & 1] = f2_add(sum2[j & 1], f2_pack(p0, p1));
-        pk[j] = F16 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
-      }
-      tmem_st16(s_addr + k * 32 + u * 16, pk);
+    for (int j = 0; j < 16; ++j) {
+      float x0, x1;
+      f2_unpack(f2_fma(f2_pack(__uint_as_float(x[2 * j]), __uint_as_float(x[2 * j + 1])), cs2, nm2), x0, x1);
+      const float p0 = ex2(x0), p1 = ex2(x1);
+      sum2[j & 1] = f2_add(sum2[j & 1], f2_pack(p0, p1));
+      pk[j] = F16 ? pack_f16x2(p0, p1) : pack_bf16x2(p0, p1);
     }
+    tmem_st16(s_addr + k * 16, pk);
   }
   float a0, a1;
   f2_unpack(f2_add(sum2[0], sum2[1]), a0, a1);
@@ -980,7 +973,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_const
         if (LOCAL && need_mask) {
           const LocalBlock lb(ti, i, A.sinks);
           const RowMask mask{tok_lim - A.window + 1, tok_lim, lb.sink};
-          const int w0 = lb.k0 / 4, w1 = (lb.k1 + 3) / 4;
+          const int w0 = lb.k0 / 2, w1 = (lb.k1 + 1) / 2;
           rescale(masked_max(s_addr, mask, w0, w1) * cs_all);
           l += masked_exp<FP8>(s_addr, mask, w0, w1, cs_all, m == -INFINITY ? 0.f : -m);
           tmem_wait_st();
