@@ -55,7 +55,7 @@ struct fp2_plan {
   int64_t split_units_cap, ws_unit_seg, ws_unit_split, ws_seg_split, ws_part_ml, ws_part_o;
   EncodeTiledFn encode;
   int32_t last_launches;
-  bool attrs_set;
+  bool attrs_set, window_attrs_set[2];   // (of the kernels with and without widening)
 };
 
 // FP8 attention with V as F16 in the workspace, or widened by the kernel in every iteration?  The copy takes about 6 us and
@@ -121,7 +121,7 @@ extern "C" fp2_status fp2_plan_create(const fp2_params* p, const int32_t* h_cu, 
   pl->nblk_tot = nblk_tot;
   pl->d_table = nullptr;
   pl->last_launches = 0;
-  pl->attrs_set = false;
+  pl->attrs_set = pl->window_attrs_set[0] = pl->window_attrs_set[1] = false;
 
   // segment table: seg = Hkv * tile_off[b] + h * ntiles_b + t
   std::vector<SegInfo> segs((size_t)pl->nseg);
@@ -416,13 +416,6 @@ static auto pair_kernel(const DevParams& d) -> decltype(&score_pair_kernel<false
   return score_pair_kernel<true, 0>;
 }
 
-// The kernel of fp2_window_prefill; widen: see use_v16.
-static auto window_kernel(const fp2_plan* pl, bool widen) -> decltype(&sparse_attn_kernel<false, false, true>) {
-  if (!pl->dev.fp8) return sparse_attn_kernel<false, false, true>;
-  return widen ? sparse_attn_kernel<true, true, true> : sparse_attn_kernel<true, false, true>;
-}
-static int attn_smem(const fp2_plan* pl) { return pl->dev.fp8 ? AttnCfg<true>::kSmemBytes : AttnCfg<false>::kSmemBytes; }
-
 static fp2_status set_attrs(fp2_plan* pl) {
   if (pl->attrs_set) return FP2_OK;
   if (cudaFuncSetAttribute(pair_kernel(pl->dev), cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmemBytes) != cudaSuccess ||
@@ -435,9 +428,7 @@ static fp2_status set_attrs(fp2_plan* pl) {
       cudaFuncSetAttribute(sparse_attn_kernel<true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                            AttnCfg<true>::kSmemBytes) != cudaSuccess ||
       cudaFuncSetAttribute(sparse_attn_kernel<true, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                           AttnCfg<true>::kSmemBytes) != cudaSuccess ||
-      cudaFuncSetAttribute(window_kernel(pl, true), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(pl)) != cudaSuccess ||
-      cudaFuncSetAttribute(window_kernel(pl, false), cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(pl)) != cudaSuccess)
+                           AttnCfg<true>::kSmemBytes) != cudaSuccess)
     return FP2_ERR_CUDA;
   // The attention kernels move registers between warps with setmaxnreg, whose wait is unbounded: launch only
   // if the compiled kernels really own the registers the move assumes.
@@ -448,10 +439,6 @@ static fp2_status set_attrs(fp2_plan* pl) {
   if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
   if (cudaFuncGetAttributes(&fa, sparse_attn_kernel<true, true, false>) != cudaSuccess) return FP2_ERR_CUDA;
   if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
-  for (int widen = 0; widen < 2; ++widen) {
-    if (cudaFuncGetAttributes(&fa, window_kernel(pl, widen != 0)) != cudaSuccess) return FP2_ERR_CUDA;
-    if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
-  }
   pl->attrs_set = true;
   return FP2_OK;
 }
@@ -720,6 +707,26 @@ extern "C" fp2_status fp2_dense_prefill(fp2_plan* pl, const void* q, const void*
   return run_attention(pl, q, k, v, pt, cu, lk, nullptr, nullptr, qs, ks, vs, out, lse, workspace, false, stream);
 }
 
+// The kernel of fp2_window_prefill; widen: see use_v16.
+static auto window_kernel(const fp2_plan* pl, bool widen) -> decltype(&sparse_attn_kernel<false, false, true>) {
+  if (!pl->dev.fp8) return sparse_attn_kernel<false, false, true>;
+  return widen ? sparse_attn_kernel<true, true, true> : sparse_attn_kernel<true, false, true>;
+}
+static int attn_smem(const fp2_plan* pl) { return pl->dev.fp8 ? AttnCfg<true>::kSmemBytes : AttnCfg<false>::kSmemBytes; }
+
+// (apart from set_attrs: plans that never ask for a window should not pay for it)
+static fp2_status set_window_attrs(fp2_plan* pl, bool widen) {
+  if (pl->window_attrs_set[widen]) return FP2_OK;
+  auto kernel = window_kernel(pl, widen);
+  cudaFuncAttributes fa;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(pl)) != cudaSuccess ||
+      cudaFuncGetAttributes(&fa, kernel) != cudaSuccess)
+    return FP2_ERR_CUDA;
+  if (fa.numRegs * AttnCfg<true>::kThreads < AttnCfg<true>::kRegsAfterMove) return FP2_ERR_UNSUPPORTED;
+  pl->window_attrs_set[widen] = true;
+  return FP2_OK;
+}
+
 // Sliding window and sinks: two launches, the second the attention kernel's LOCAL form.
 extern "C" fp2_status fp2_window_prefill(fp2_plan* pl, const void* q, const void* k, const void* v, const int32_t* pt,
                                          const int32_t* cu, const int32_t* lk, const float* qs, const float* ks, const float* vs,
@@ -737,6 +744,7 @@ extern "C" fp2_status fp2_window_prefill(fp2_plan* pl, const void* q, const void
   // iterations of a segment: the blocks of the first row's window and of the rows behind it, and of the sinks
   const int64_t per_seg = (int64_t)(window + kTileRows - 2) / kBlock + 2 + (sinks + kBlock - 1) / kBlock;
   const bool use_v16 = pl->dev.fp8 && std::min(pl->idx_capacity, pl->nseg * per_seg) >= pl->v16_iters;
+  if ((s = set_window_attrs(pl, !use_v16)) != FP2_OK) return s;
   int32_t* const counter = reinterpret_cast<int32_t*>(ws + pl->ws_counter);
   // Clears the work counter; FP8: V as F16.  What it finds of missing pages is not reported (words of the counter block that
   // nothing reads): the attention kernel reports those that a query sees.

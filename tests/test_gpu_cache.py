@@ -577,3 +577,31 @@ def test_offsets_beyond_32_bits(fmt):
     ro, _, mass, _ = attend(q.cpu(), got[0], got[1], 149, 0, 0)
     assert bool(((out.double().cpu() - ro).abs() <= 2.0 ** -8 * ro.abs() + 2.0 ** -9 * mass).all())
     assert binding.fp2_cache_read_status(cache, ws)[0] == 0
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+@pytest.mark.parametrize("hq,hkv,page,lens,lq", [(64, 1, 16, [500, 77], [3, 1]), (40, 8, 8, [333], [2]), (5, 5, 32, [200, 3], [150, 3]),
+                                                 (8, 2, 16, [700], [700])])
+def test_decode_many_rows(fmt, hq, hkv, page, lens, lq):
+    """More packed rows than one tile holds: wide groups, many queries, a whole prompt."""
+    st = Store(fmt, lens, hq, hkv, page, seed=11)
+    q = queries(st.rng, sum(lq), hq)
+    for window, sinks in [(0, 0), (90, 20)]:
+        out, lse = st.decode(q, lq, window, sinks)
+        check(st, q, lq, out, lse, window, sinks)
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_sequences_that_share_a_prefix(fmt):
+    """Two sequences with the same full pages in front: appending to each leaves these alone, both read them."""
+    st = Store(fmt, [64, 64], 8, 2, 16, seed=12, capacity=[100, 100])
+    st.pt[1, :4] = st.pt[0, :4]
+    st.dpt = torch.from_numpy(st.pt).cuda()
+    shared = st.dk[[int(p) for p in st.pt[0, :4]]].clone()
+    x = torch.from_numpy(st.rng.normal(0, 3, (50, 4, D))).bfloat16().cuda()
+    lens, news = [64 + 20, 64 + 30], [20, 30]
+    run_append(st, x[:, :2], x[:, 2:], lens, news)
+    assert same(st.dk[[int(p) for p in st.pt[0, :4]]], shared)
+    q = queries(st.rng, 2, 8)
+    out, lse = st.decode(q, [1, 1], lens=lens)
+    check(st, q, [1, 1], out, lse, 0, 0, lens=lens)
