@@ -49,10 +49,15 @@ __device__ __forceinline__ float page_scale_for(uint32_t amax_bits) {
 // Number of page slots reserved in front of sequence b's: its n new tokens touch at most n / p + 2 pages.
 __device__ __forceinline__ long long append_slot0(int cu, int b, int shift) { return (long long)(cu >> shift) + 2ll * b; }
 
-// Maximum of the magnitudes of BF16 pairs (a NaN loses against a number; NaN against NaN stays)
+// Maximum of the magnitudes of BF16 pairs, whatever its signs (a NaN loses against a number; NaN against NaN stays)
 __device__ __forceinline__ uint32_t max_abs_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;
-  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b & 0x7fff7fffu));
+  asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 
@@ -167,7 +172,7 @@ cache_append_kernel(AppendArgs A) {
       uint32_t m = 0;
 #pragma unroll
       for (int i = 0; i < kRows / 2; ++i) m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(m, x[i].x), x[i].y), x[i].z), x[i].w);
-      uint32_t amax = max(m & 0xffffu, m >> 16);
+      uint32_t amax = max(m & 0x7fffu, (m >> 16) & 0x7fffu);
       if (__any_sync(0xffffffffu, amax >= 0x7f80u)) {      // an infinity, or nothing but NaN: the finite ones count
         amax = 0;
 #pragma unroll
@@ -215,6 +220,9 @@ cache_append_kernel(AppendArgs A) {
     const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0u, usual = scale >= 0x1p-100f && scale <= 0x1p126f;
     const float inv = 1.0f / scale, inv_lo = inv * (1.f - 0x1p-21f), inv_hi = inv * (1.f + 0x1p-21f);
     auto quantise = [&](uint32_t w, float f) { return pack_e4m3x2(bf16_lo(w) * f, bf16_hi(w) * f); };
+    // (the product with a power of two is a BF16 number, but for subnormals, which e4m3 rounds to zero)
+    const uint32_t inv2 = (__float_as_uint(inv) >> 16) * 0x10001u;
+    auto quantise_pow2 = [&](uint32_t w) { const uint32_t s = mul_bf16x2(w, inv2); return pack_e4m3x2(bf16_lo(s), bf16_hi(s)); };
 #pragma unroll
     for (int i = 0; i < kRows / 2; ++i) {
       if (!((live >> i) & 1u)) continue;
@@ -222,7 +230,7 @@ cache_append_kernel(AppendArgs A) {
       uint32_t o[4];
       if (pow2 && usual) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = quantise(w[k], inv);
+        for (int k = 0; k < 4; ++k) o[k] = quantise_pow2(w[k]);
       } else {
         uint32_t differ = usual ? 0u : 1u;
 #pragma unroll
