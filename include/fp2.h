@@ -292,8 +292,8 @@ typedef struct {
   float softmax_scale;    /* 0 selects 1 / sqrt(head_dim)                                             */
 } fp2_cache_params;
 
-/* Host only; FP2_ERR_INVALID_ARG / _UNSUPPORTED / _CAPACITY (a sequence of more than 2^30 tokens) for shapes that are not
- * handled.  Without a usable CUDA device the handle is returned, but calls on it return FP2_ERR_CUDA. */
+/* Host only; FP2_ERR_INVALID_ARG / _UNSUPPORTED / _CAPACITY (sequences of more than 2^30 tokens, a pool of 2^31 slots, more than
+ * 8192 query heads) for shapes that are not handled.  Without a usable CUDA device the handle is returned, but calls on it return FP2_ERR_CUDA. */
 fp2_status fp2_cache_create(const fp2_cache_params* params, fp2_cache** out);
 void fp2_cache_destroy(fp2_cache* cache);
 

@@ -148,3 +148,15 @@ def test_window_prefill_refuses(window, sinks, code):
         assert lib.fp2_window_prefill(plan.handle, a["q"], p, p, a["pt"], p, p, a["qs"], p, p, 16, 0, a["out"], None, a["ws"], None) == 1
     assert lib.fp2_window_prefill(None, p, p, p, p, p, p, p, p, p, 16, 0, p, None, p, None) == 1
     plan.close()
+
+
+@pytest.mark.parametrize("kw,code", [(dict(num_pages=1 << 27), 3), (dict(num_pages=(1 << 27) - 1), None), (dict(num_pages=1 << 24, page_size=128), 3),
+                                     (dict(max_pages_per_seq=1 << 26), None), (dict(num_q_heads=8192, num_kv_heads=1), None),
+                                     (dict(num_q_heads=8200, num_kv_heads=1), 3)])
+def test_cache_create_at_its_limits(kw, code):
+    if code is None:
+        binding.Cache(cache_params(**kw)).close()
+        return
+    with pytest.raises(binding.Fp2Error) as e:
+        binding.Cache(cache_params(**kw))
+    assert e.value.code == code

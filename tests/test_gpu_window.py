@@ -195,3 +195,17 @@ def test_window_next_to_the_other_stage_calls_on_one_workspace(fp8):
     assert torch.equal(o.view(torch.int16), ref.view(torch.int16)) and torch.equal(l, ref_l)
     binding.fp2_read_status(p.plan, p.ws)
     binding.fp2_read_status(p.plan, ws)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_window_tokens_behind_a_tile_do_not_matter(fp8):
+    """The newest tokens hold NaN: the queries that see them get NaN, those of earlier 128-row tiles (32 queries here) are as before."""
+    p = Prompt(fp8, [(600, 600)], 8, 2, 16, seed=13)
+    clean, clean_l = p.run(100, 4)
+    for tok in (590, 599):
+        for x in (p.k, p.v):
+            x.view(-1, 2, D)[int(p.pt[0, tok // 16]) * 16 + tok % 16] = NAN8 if fp8 else math.nan
+    out, lse = p.run(100, 4)
+    assert torch.equal(out[:576].view(torch.int16), clean[:576].view(torch.int16)) and torch.equal(lse[:, :576], clean_l[:, :576])
+    assert bool(torch.isnan(out[590:].float()).all()) and bool(torch.isnan(lse[:, 590:]).all())
+    binding.fp2_read_status(p.plan, p.ws)
