@@ -516,6 +516,12 @@ class DeviceCase:
                           self.seqlens_k, self.q_scale, self.k_scale, self.v_scale, self.out, self.lse,
                           self.workspace)
 
+    def window(self, window_tokens, sink_tokens=0):
+        self._poison_outputs()
+        fp2_window_prefill(self.plan, self.q, self.k_cache, self.v_cache, self.page_table, self.cu_seqlens_q, self.seqlens_k,
+                           self.q_scale, self.k_scale, self.v_scale, window_tokens, sink_tokens, self.out, self.lse,
+                           self.workspace)
+
     def export_csr(self, tile_tokens=64):
         """(cu, idx) device tensors of the lists currently in the buffers."""
         cu = torch.empty(self.plan.num_segments + 1, dtype=torch.int32, device=self.q.device)

@@ -19,11 +19,11 @@
 // (By TMA, a box per page and operand, lanes in turn: everything 4 to 6 % slower.)
 //
 // Measured, whole calls: 64 sequences of 4096 tokens, 8 KV heads, 168 us in BF16 (6.4 TB/s, 0.98 of the copy rate), 100 us in 8 bits
-// (5.4 TB/s, 0.82: four warps a CTA issue 41 % of the time, and what a warp does on a step takes longer than its bytes); 131072
-// tokens of 4 heads 52 us in BF16, of which 41 are the bytes, 5 the start and 5 the joining of 74 parts per head.
+// (5.4 TB/s, 0.82; 37 sequences of 8192 tokens, a whole unit per CTA, 6.2 TB/s: the rest is the units' ends, 2.5 parts per CTA);
+// 131072 tokens of 4 heads 52 us in BF16, of which 41 are the bytes, 5 the start and 5 the joining of 74 parts per head.
 //
 // S^T = K Q^T and O^T += V^T P^T are m16n8k16 MMAs of a warp with the tokens (then the dims) as the long side and 8 packed
-// (token, query head) rows of the KV head as the short one, NR times: a group of up to eight heads wastes nothing.  What tcgen05
+// (token, query head) rows of the KV head as the short one, NR times: a group of eight heads fills it.  What tcgen05
 // would add in rate is not what bounds this, and its 64 rows are what such a group has no use for.  K and V are read from shared
 // memory 16 bytes a lane; which of a lane's values play which index of the contraction over dims in K Q^T, or which row (a dim) of
 // V^T, is free as long as Q is permuted alike and O stored accordingly, so nothing is transposed but P (8 x 8 at a time, one

@@ -605,3 +605,55 @@ def test_sequences_that_share_a_prefix(fmt):
     q = queries(st.rng, 2, 8)
     out, lse = st.decode(q, [1, 1], lens=lens)
     check(st, q, [1, 1], out, lse, 0, 0, lens=lens)
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_local_layers_from_prompt_to_answer(fmt):
+    """A layer with a sliding window: the prompt in two chunks through fp2_window_prefill, on the cache itself (BF16, per-head scales)
+    or behind fp2_cache_expand (page scales), then tokens through fp2_decode with the same window and sinks."""
+    hq, hkv, page, window, sinks = 8, 2, 16, 90, 5
+    chunks, steps = [(200, 77), (150, 301)], 3
+    total = [sum(c[b] for c in chunks) for b in range(2)]
+    st = Store(fmt, [0, 0], hq, hkv, page, seed=21 + fmt, capacity=[n + 8 for n in total])
+    rng, lens = st.rng, [0, 0]
+    for chunk in chunks:
+        lens = [a + n for a, n in zip(lens, chunk)]
+        n = sum(chunk)
+        x = torch.from_numpy(rng.normal(0, 1, (n, 2 * hkv, D))).bfloat16().cuda()
+        q, q_scale = queries(rng, n, hq), None
+        run_append(st, x[:, :hkv], x[:, hkv:], lens, list(chunk))
+        lk = torch.tensor(lens, dtype=torch.int32).cuda()
+        k, v, ks, vs = st.dk, st.dv, st.dks, st.dvs
+        qv = q
+        if fmt == 1:      # an FP8 plan takes e4m3 queries
+            q_scale = torch.full((hq,), 1.0 / 64, device="cuda")
+            qv = (q.float() * 64).clamp(-448, 448).to(E4M3).view(torch.uint8)
+            q = qv.view(E4M3).float().cpu() / 64
+        elif fmt == 2:
+            k, v = (torch.zeros(st.pool, page, hkv, D, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+            binding.fp2_cache_expand(st.cache, st.dk, st.dv, st.dpt, lk, ks, vs, k, v, st.dpt, st.ws)
+            ks = vs = None
+        cu = [0, chunk[0], n]
+        plan = binding.Plan(dict(num_seqs=2, total_q=n, num_q_heads=hq, num_kv_heads=hkv, head_dim=D, block_size=128, tile_rows=128,
+                                 page_size=page, num_pages=st.pool, max_pages_per_seq=st.mp, sink_tokens=256, window_tokens=512,
+                                 use_correction=1, alpha=0.1, softmax_scale=0.0, dtype=1 if fmt == 1 else 0), cu, lens)
+        out, lse = torch.empty(n, hq, D, dtype=torch.bfloat16, device="cuda"), torch.empty(hq, n, device="cuda")
+        ws = plan.new_workspace()
+        binding.fp2_window_prefill(plan, qv, k, v, st.dpt, torch.tensor(cu, dtype=torch.int32).cuda(), lk, q_scale, ks, vs, window,
+                                   sinks, out, lse, ws)
+        binding.fp2_read_status(plan, ws)
+        for b in range(2):
+            kk, vv = st.tokens(b, lens[b])
+            ro, rl, mass, _ = attend(q[cu[b]:cu[b + 1]].cpu(), kk, vv, lens[b] - chunk[b], window, sinks)
+            # probabilities rounded to BF16 or F16 (2^-8 at most), logits and sums as in close() far below that, the output once
+            err = (out[cu[b]:cu[b + 1]].double().cpu() - ro).abs()
+            assert bool((err <= 2.0 ** -8 * ro.abs() + 1.1 * 2.0 ** -8 * mass).all())
+            assert float((lse[:, cu[b]:cu[b + 1]].double().cpu() - rl).abs().max()) <= 1e-3
+    for _ in range(steps):
+        lens = [a + 1 for a in lens]
+        x = torch.from_numpy(rng.normal(0, 1, (2, 2 * hkv, D))).bfloat16().cuda()
+        q = queries(rng, 2, hq)
+        run_append(st, x[:, :hkv], x[:, hkv:], lens, [1, 1])
+        out, lse = st.decode(q, [1, 1], window, sinks, lens=lens)
+        check(st, q, [1, 1], out, lse, window, sinks, lens=lens)
+    assert binding.fp2_cache_read_status(st.cache, st.ws)[0] == 0

@@ -209,3 +209,21 @@ def test_window_tokens_behind_a_tile_do_not_matter(fp8):
     assert torch.equal(out[:576].view(torch.int16), clean[:576].view(torch.int16)) and torch.equal(lse[:, :576], clean_l[:, :576])
     assert bool(torch.isnan(out[590:].float()).all()) and bool(torch.isnan(lse[:, 590:]).all())
     binding.fp2_read_status(p.plan, p.ws)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8"])
+def test_window_on_the_oracles_inputs(dtype):
+    """The generator's inputs (locality, sinks, vertical keys) through the helper of the other stage calls, against the oracle's dense
+    path where the window covers everything."""
+    from oracle import fp2_oracle as O
+    from paper_2608_19758_b200 import inputs
+    spec = inputs.small_spec(seqs=[(700, 100), (300, 0)], num_q_heads=8, num_kv_heads=2, page_size=16, config_id=97, dtype=dtype)
+    case = inputs.make_case(spec)
+    dc = binding.DeviceCase(case)
+    dc.poison = True
+    dc.window(1 << 20)
+    dc.status()
+    wl = O.Workload(O.Params.from_dict(case.params()), **inputs.oracle_args(case))
+    ref, lref = O.scatter_output(wl, O.oracle_attend(wl, None, dense=True), case.total_q)
+    assert np.abs(dc.out.float().cpu().numpy() - ref).max() <= (2e-2 if dtype == "bf16" else 6e-2)     # the stage calls' tolerances
+    assert (np.abs(dc.lse.cpu().numpy() - lref) / np.maximum(np.abs(lref), 1)).max() <= 1e-3
