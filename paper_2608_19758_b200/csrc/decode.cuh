@@ -33,8 +33,10 @@
 // F16 after a power of two per row has brought its maximum to 2^13 .. 2^14 (elements 2^-28 below it round); P as F16 against a
 // reference 8 binades below the running maximum, where the steps are 2^-11 relative down to 2^-22 of the maximum.  Sums in 32 bits.
 // (The warp-level MMA takes e4m3 operands as such, Q as a pair of them; K Q^T then took twice the instructions: it widens them itself.)
-// Scales per page: ks multiplies the logits; vs enters P, in the exponent, so that P V needs none:
-// y = x + log2 vs has the running maximum, p = 2^(y - m), and l adds p / vs.
+// Scales per page: ks multiplies the logits; vs enters P, in the exponent, so that P V needs none: y = x + log2 vs has the running
+// maximum of P, p = 2^(y - m).  The sum of the weights has a reference of its own, l = sum 2^(x - e): scales may lie 2^200 and more
+// apart (2^-100 is the writer's for a page of zeros), so what y hides can be the whole of l, and 2^-m is no unit for it.
+// (64 ragged sequences of 8-bit pages: 96.5 us with l taken back from P, p / vs, which loses weights and leaves fp32; 98.0 so.)
 #pragma once
 #include <cuda_bf16.h>
 #include "common.cuh"
@@ -85,7 +87,7 @@ struct DecodeArgs {
   __nv_bfloat16* out;
   float* lse;
   float* part_o;                // [2 grid][8 NR][128]
-  float2* part_ml;              // [2 grid][8 NR]
+  void* part_ml;                // [2 grid][8 NR] RowState
   int32_t* counters;            // [3][grid], zero between calls: parts of a unit's first group, of a later group, groups of a unit
   int* status;
   int32_t total_q, num_q_heads, group, window, sinks;
@@ -93,6 +95,26 @@ struct DecodeArgs {
   float scale_log2;
   CacheGeom g;
 };
+
+// What goes with a row's O: its references and its sum, out = O 2^(m - e) / l, lse = e + log2 l.  Without scales per page e is m.
+template <bool OWN_E> struct RowState;
+template <> struct alignas(8) RowState<false> {
+  float m, l;
+  static __device__ __forceinline__ RowState none() { return {-INFINITY, 0.f}; }
+  __device__ __forceinline__ float e() const { return m; }
+  __device__ __forceinline__ void set_e(float) {}
+  __device__ __forceinline__ void store_cg(void* p, long long i) const { __stcg((float2*)p + i, make_float2(m, l)); }
+  static __device__ __forceinline__ RowState load_cg(const void* p, long long i) { const float2 v = __ldcg((const float2*)p + i); return {v.x, v.y}; }
+};
+template <> struct alignas(16) RowState<true> {
+  float m, l, own, unused;
+  static __device__ __forceinline__ RowState none() { return {-INFINITY, 0.f, -INFINITY, 0.f}; }
+  __device__ __forceinline__ float e() const { return own; }
+  __device__ __forceinline__ void set_e(float x) { own = x; }
+  __device__ __forceinline__ void store_cg(void* p, long long i) const { __stcg((float4*)p + i, make_float4(m, l, own, 0.f)); }
+  static __device__ __forceinline__ RowState load_cg(const void* p, long long i) { const float4 v = __ldcg((const float4*)p + i); return {v.x, v.y, v.z, 0.f}; }
+};
+constexpr int kRowStateBytes = sizeof(RowState<true>);
 
 // One sequence's share of the work
 struct DecodeSeq {
@@ -186,7 +208,8 @@ template <int FMT, int NR>
 __global__ void __launch_bounds__(kDecThreads, kDecCtasPerSm)
 decode_kernel(DecodeArgs A) {
   using Cfg = DecodeCfg<FMT, NR>;
-  constexpr bool FP8 = Cfg::kFp8;
+  constexpr bool FP8 = Cfg::kFp8, OWN_E = FMT == FMT_FP8_PAGE;
+  using State = RowState<OWN_E>;
   constexpr int RT = Cfg::kRows, ST = Cfg::kStages, TOK = Cfg::kTok;
   constexpr int G = TOK / 8;             // groups of eight tokens of a step: what a page holds at least
   constexpr uint32_t kAllLive = TOK == 32 ? 0xffffffffu : (1u << TOK) - 1u;
@@ -194,7 +217,7 @@ decode_kernel(DecodeArgs A) {
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~uintptr_t(127));
   __shared__ float page_scales[kDecWarps][ST][2 * G];      // PAGE: ks of the groups, then vs
   __shared__ uint32_t live_s[kDecWarps][ST];               // tokens of the step that were copied
-  __shared__ float2 ml_s[kDecWarps][RT];
+  __shared__ State ml_s[kDecWarps][RT];
   __shared__ long long scan_s[kDecWarps];
   __shared__ long long found_base;                         // (the sequence that the share begins in, what is in front of it)
   __shared__ int found_b, last_s;
@@ -487,12 +510,15 @@ decode_kernel(DecodeArgs A) {
 
     float o[NR][8][4];                   // tile t: rows 2 c, 2 c + 1 of two dims of this lane's
     float m[NR][2], l[NR][2];
+    float e[OWN_E ? NR : 1][2];          // (else m)
+    (void)e;
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
 #pragma unroll
       for (int t = 0; t < 8; ++t) o[n][t][0] = o[n][t][1] = o[n][t][2] = o[n][t][3] = 0.f;
       m[n][0] = m[n][1] = -INFINITY;
       l[n][0] = l[n][1] = 0.f;
+      if constexpr (OWN_E) e[n][0] = e[n][1] = -INFINITY;
     }
 
     // ------------------------------ steps ------------------------------
@@ -539,17 +565,16 @@ decode_kernel(DecodeArgs A) {
           }
         }
       }
-      float kmul[G], vlog[G], vinv[G];
+      float vlog[G];
+      if constexpr (OWN_E) {
 #pragma unroll
-      for (int j = 0; j < G; ++j) {
-        kmul[j] = 1.f;
-        vlog[j] = 0.f;
-        vinv[j] = 1.f;
-        if constexpr (FMT == FMT_FP8_PAGE) {
-          kmul[j] = page_scales[warp][now][j];
-          const float vs = page_scales[warp][now][G + j];
-          vlog[j] = vs > 0.f ? __log2f(vs) : 0.f;
-          vinv[j] = vs > 0.f ? __frcp_rn(vs) : 0.f;
+        for (int j = 0; j < G; ++j) {
+          const float ks = page_scales[warp][now][j], vs = page_scales[warp][now][G + j];
+          vlog[j] = vs > 0.f ? __log2f(vs) : 0.f;      // (0: nothing of the group was copied)
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) x[n][j / 2][(j & 1) * 2 + v] *= cs[n][v] * ks;
         }
       }
       if (!(live == kAllLive && t0 + TOK - 1 <= u.pmin && (A.window <= 0 || t0 > u.pmax - A.window || t0 + TOK - 1 < A.sinks))) {
@@ -566,8 +591,21 @@ decode_kernel(DecodeArgs A) {
             }
           }
       }
-      // y = x mul + log2 vs.  m is the reference of the exponentials: 8 below the maximum when it was set, moved when a row has
+      // y = x mul (+ log2 vs).  m is the reference of the exponentials: 8 below the maximum when it was set, moved when a row has
       // outgrown it by 14 (F16 holds 2^15).  Lanes look at their own tokens; only a move needs the row's maximum.
+      auto row_max = [](float a) {
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
+        a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
+        return fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
+      };
+      auto move_e = [&](int n, int v) {  // l's own reference: to the maximum of x
+        float a = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < G; ++j) a = fmaxf(a, x[n][j / 2][(j & 1) * 2 + v]);
+        const float en = fmaxf(e[n][v], row_max(a));
+        l[n][v] *= en == e[n][v] ? 1.f : ex2(e[n][v] - en);
+        e[n][v] = en;
+      };
       float my[NR][2];                   // this lane's maxima
       bool outgrown = false;
 #pragma unroll
@@ -578,10 +616,9 @@ decode_kernel(DecodeArgs A) {
 #pragma unroll
           for (int j = 0; j < G; ++j) {
             const float y = x[n][j / 2][(j & 1) * 2 + v];
-            if constexpr (FMT == FMT_FP8_PAGE) a = fmaxf(a, fmaf(y, fmaxf(cs[n][v] * kmul[j], 1e-37f), vlog[j]));
-            else a = fmaxf(a, y);
+            a = fmaxf(a, OWN_E ? y + vlog[j] : y);
           }
-          my[n][v] = FMT == FMT_FP8_PAGE ? a : a * cs[n][v];
+          my[n][v] = OWN_E ? a : a * cs[n][v];
           outgrown |= my[n][v] > m[n][v] + 14.f;
         }
       if (__any_sync(0xffffffffu, outgrown)) {
@@ -589,20 +626,49 @@ decode_kernel(DecodeArgs A) {
         for (int n = 0; n < NR; ++n)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            float a = my[n][v];
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 4));
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
-            a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
-            const float mn = fmaxf(m[n][v], a - 8.f);
+            const float mn = fmaxf(m[n][v], row_max(my[n][v]) - 8.f);
             const float f = mn == m[n][v] ? 1.f : ex2(m[n][v] - mn);
             m[n][v] = mn;
-            l[n][v] *= f;
+            if constexpr (OWN_E) move_e(n, v);
+            else l[n][v] *= f;
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
               o[n][t][v] *= f;
               o[n][t][2 + v] *= f;
             }
           }
+      }
+      if constexpr (OWN_E) {
+        // Weights against e, which a row may outgrow without outgrowing m (large weights on small values): then it moves first.
+        auto weights = [&](int n, int v) {
+          const float ref = e[n][v] == -INFINITY ? 0.f : e[n][v];
+          float sum = 0.f;
+#pragma unroll
+          for (int j = 0; j < G; ++j) sum += ex2(x[n][j / 2][(j & 1) * 2 + v] - ref);
+          return sum;
+        };
+        float add[NR][2];
+        bool large = false;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            add[n][v] = weights(n, v);
+            large |= add[n][v] > 0x1p30f;
+          }
+        if (__any_sync(0xffffffffu, large)) {
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              move_e(n, v);
+              add[n][v] = weights(n, v);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) l[n][v] += add[n][v];
       }
       uint32_t pb[NR][G], pl[FP8 ? 1 : NR][G];     // P^T: rows l4, tokens 8 j + 2 c, + 1
       (void)pl;
@@ -616,9 +682,13 @@ decode_kernel(DecodeArgs A) {
           float p[2];
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            const float mul = FMT == FMT_FP8_PAGE ? fmaxf(cs[n][v] * kmul[j], 1e-37f) : cs[n][v];
-            p[v] = ex2(fmaf(x[n][j / 2][(j & 1) * 2 + v], mul, vlog[j] - ref[v]));
-            l[n][v] = FMT == FMT_FP8_PAGE ? fmaf(p[v], vinv[j], l[n][v]) : l[n][v] + p[v];
+            const float xj = x[n][j / 2][(j & 1) * 2 + v];
+            if constexpr (OWN_E) {
+              p[v] = ex2(xj + (vlog[j] - ref[v]));
+            } else {
+              p[v] = ex2(fmaf(xj, cs[n][v], -ref[v]));
+              l[n][v] += p[v];
+            }
           }
           if constexpr (FP8) {
             pb[n][j] = transpose8(pack_f16x2(p[0], p[1]));
@@ -689,7 +759,11 @@ decode_kernel(DecodeArgs A) {
         ls += __shfl_xor_sync(0xffffffffu, ls, 8);
         ls += __shfl_xor_sync(0xffffffffu, ls, 16);
         const int row = n * 8 + 2 * c + v;
-        if (l4 == 0) ml_s[warp][row] = make_float2(m[n][v], ls);
+        State sum = State::none();
+        sum.m = m[n][v];
+        sum.l = ls;
+        if constexpr (OWN_E) sum.set_e(e[n][v]);
+        if (l4 == 0) ml_s[warp][row] = sum;
         float* const orow = osm(warp) + row * 128;
 #pragma unroll
         for (int t = 0; t < 8; t += 2) {
@@ -704,17 +778,20 @@ decode_kernel(DecodeArgs A) {
       __syncthreads();
       for (int k = tid; k < u.nrows * 32; k += kDecThreads) {
         const int row = k >> 5, pc = k & 31;
-        float M = -INFINITY, L = 0.f;
+        State sum = State::none();
 #pragma unroll
-        for (int w = 0; w < kDecWarps; ++w) M = fmaxf(M, ml_s[w][row].x);
-        const float ref = M == -INFINITY ? 0.f : M;
+        for (int w = 0; w < kDecWarps; ++w) {
+          sum.m = fmaxf(sum.m, ml_s[w][row].m);
+          sum.set_e(fmaxf(sum.e(), ml_s[w][row].e()));
+        }
+        const float ref = sum.m == -INFINITY ? 0.f : sum.m, ref_e = sum.e() == -INFINITY ? 0.f : sum.e();
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kDecWarps; ++w) {
-          const float2 ml = ml_s[w][row];
-          const float f = ex2(ml.x - ref);
+          const State part = ml_s[w][row];
+          const float f = ex2(part.m - ref);
           const float4 v = *reinterpret_cast<const float4*>(osm(w) + row * 128 + piece(row, pc) * 4);
-          L = fmaf(f, ml.y, L);
+          sum.l = fmaf(OWN_E ? ex2(part.e() - ref_e) : f, part.l, sum.l);
           acc.x = fmaf(f, v.x, acc.x);
           acc.y = fmaf(f, v.y, acc.y);
           acc.z = fmaf(f, v.z, acc.z);
@@ -724,16 +801,21 @@ decode_kernel(DecodeArgs A) {
           int tok, head;
           row_of(u, row, tok, head);
           const size_t at = (size_t)(u.c0 + tok);
-          const float inv = L > 0.f ? out_scale / L : L == 0.f ? 0.f : NAN;
+          const float inv = sum.l > 0.f ? out_scale / sum.l : sum.l == 0.f ? 0.f : NAN;
+          acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+          if constexpr (OWN_E) {         // times 2^(m - e), in halves: the whole may be out of range where the result is not
+            const float h = ex2(0.5f * (ref - ref_e));
+            acc = make_float4(acc.x * h * h, acc.y * h * h, acc.z * h * h, acc.w * h * h);
+          }
           uint2 w;
-          w.x = pack_bf16x2(acc.x * inv, acc.y * inv);
-          w.y = pack_bf16x2(acc.z * inv, acc.w * inv);
+          w.x = pack_bf16x2(acc.x, acc.y);
+          w.y = pack_bf16x2(acc.z, acc.w);
           *reinterpret_cast<uint2*>(A.out + (at * A.num_q_heads + head) * kHeadDim + pc * 4) = w;
           if (pc == 0 && A.lse != nullptr)
-            A.lse[(size_t)head * A.total_q + at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+            A.lse[(size_t)head * A.total_q + at] = sum.l == 0.f ? -INFINITY : (sum.e() + log2f(sum.l)) * 0.6931471805599453f;
         } else {
           __stcg(reinterpret_cast<float4*>(A.part_o + (place + row) * 128) + pc, acc);
-          if (pc == 0) __stcg(A.part_ml + place + row, make_float2(M, L));
+          if (pc == 0) sum.store_cg(A.part_ml, place + row);
         }
       }
     };
@@ -754,52 +836,55 @@ decode_kernel(DecodeArgs A) {
       return last_s != 0;
     };
     // n partial results, those of the CTAs w, w + step ..., by warp in turn, then over the warps as above.  Eight rows at a time, of
-    // kDecJoin of them at once: all loads of that are on their way together.
+    // kDecJoin of them at once: all loads of that are on their way together.  A lane keeps the state of one of the eight rows.
     auto join_parts = [&](int w, int step, int n, long long place) {
 #pragma unroll 1
       for (int r0 = 0; r0 < u.nrows; r0 += 8) {
-        float M[8], L[8];
+        State sum = State::none();
         float4 acc[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          M[r] = -INFINITY;
-          L[r] = 0.f;
-          acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
-        }
+        for (int r = 0; r < 8; ++r) acc[r] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
         for (int k0 = warp; k0 < n; k0 += kDecWarps * kDecJoin) {
           float4 v[kDecJoin][8];
-          float2 ml[kDecJoin][8];
+          State part[kDecJoin];
 #pragma unroll
           for (int j = 0; j < kDecJoin; ++j) {
             const int k = k0 + j * kDecWarps;
             const long long row = place_of(w + k * step) + r0;
+            part[j] = k < n && r0 + (lane & 7) < u.nrows ? State::load_cg(A.part_ml, row + (lane & 7)) : State::none();
 #pragma unroll
-            for (int r = 0; r < 8; ++r) {
-              const bool in = k < n && r0 + r < u.nrows;
-              ml[j][r] = in ? __ldcg(A.part_ml + row + r) : make_float2(-INFINITY, 0.f);
-              v[j][r] = in ? __ldcg(reinterpret_cast<const float4*>(A.part_o + (row + r) * 128) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
-            }
+            for (int r = 0; r < 8; ++r)
+              v[j][r] = k < n && r0 + r < u.nrows ? __ldcg(reinterpret_cast<const float4*>(A.part_o + (row + r) * 128) + lane)
+                                                  : make_float4(0.f, 0.f, 0.f, 0.f);
           }
 #pragma unroll
-          for (int j = 0; j < kDecJoin; ++j)
+          for (int j = 0; j < kDecJoin; ++j) {
+            const float mn = fmaxf(sum.m, part[j].m), ref = mn == -INFINITY ? 0.f : mn;
+            const float f0 = ex2(sum.m - ref), f1 = ex2(part[j].m - ref);
+            float g0 = f0, g1 = f1;
+            if constexpr (OWN_E) {
+              const float en = fmaxf(sum.e(), part[j].e()), ref_e = en == -INFINITY ? 0.f : en;
+              g0 = ex2(sum.e() - ref_e);
+              g1 = ex2(part[j].e() - ref_e);
+              sum.set_e(en);
+            }
+            sum.m = mn;
+            sum.l = fmaf(g1, part[j].l, g0 * sum.l);
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
-              const float mn = fmaxf(M[r], ml[j][r].x), ref = mn == -INFINITY ? 0.f : mn;
-              const float f0 = ex2(M[r] - ref), f1 = ex2(ml[j][r].x - ref);
-              M[r] = mn;
-              L[r] = fmaf(f1, ml[j][r].y, f0 * L[r]);
-              acc[r].x = fmaf(f1, v[j][r].x, f0 * acc[r].x);
-              acc[r].y = fmaf(f1, v[j][r].y, f0 * acc[r].y);
-              acc[r].z = fmaf(f1, v[j][r].z, f0 * acc[r].z);
-              acc[r].w = fmaf(f1, v[j][r].w, f0 * acc[r].w);
+              const float a0 = __shfl_sync(0xffffffffu, f0, r), a1 = __shfl_sync(0xffffffffu, f1, r);
+              acc[r].x = fmaf(a1, v[j][r].x, a0 * acc[r].x);
+              acc[r].y = fmaf(a1, v[j][r].y, a0 * acc[r].y);
+              acc[r].z = fmaf(a1, v[j][r].z, a0 * acc[r].z);
+              acc[r].w = fmaf(a1, v[j][r].w, a0 * acc[r].w);
             }
+          }
         }
+        if (lane < 8) ml_s[warp][r0 + lane] = sum;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          if (lane == 0) ml_s[warp][r0 + r] = make_float2(M[r], L[r]);
+        for (int r = 0; r < 8; ++r)
           *reinterpret_cast<float4*>(osm(warp) + (r0 + r) * 128 + piece(r0 + r, lane) * 4) = acc[r];
-        }
       }
       join(place);
     };

@@ -78,7 +78,7 @@ extern "C" fp2_status fp2_cache_create(const fp2_cache_params* p, fp2_cache** ou
   c->workers = std::max(sms, 1) * kDecCtasPerSm;
   int64_t o = 1024;                                        // status block
   c->ws_counters = o; o += up(12 * (int64_t)c->workers, 1024);
-  c->ws_part_ml = o;  o += up(2ll * c->workers * kMaxDecodeTileRows * 8, 1024);
+  c->ws_part_ml = o;  o += up(2ll * c->workers * kMaxDecodeTileRows * kRowStateBytes, 1024);
   c->ws_part_o = o;   o += 2ll * c->workers * kMaxDecodeTileRows * kHeadDim * 4;
   c->ws_bytes = o;
   *out = c;
@@ -218,7 +218,7 @@ extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_st
   a.out = (__nv_bfloat16*)out;
   a.lse = lse;
   a.part_o = (float*)(ws + c->ws_part_o);
-  a.part_ml = (float2*)(ws + c->ws_part_ml);
+  a.part_ml = ws + c->ws_part_ml;
   a.counters = (int32_t*)(ws + c->ws_counters);
   a.status = (int*)ws;
   a.total_q = total_q; a.num_q_heads = c->prm.num_q_heads; a.group = group;

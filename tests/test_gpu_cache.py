@@ -657,3 +657,72 @@ def test_local_layers_from_prompt_to_answer(fmt):
         out, lse = st.decode(q, [1, 1], window, sinks, lens=lens)
         check(st, q, [1, 1], out, lse, window, sinks, lens=lens)
     assert binding.fp2_cache_read_status(st.cache, st.ws)[0] == 0
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# scales of pages at the ends of their range
+# ---------------------------------------------------------------------------------------------------------------------
+PAGE_SCALES = [
+    # exponents of V's scales, page by page in turn; None: a page of zeros, at the writer's 2^-100
+    [None, 36], [-120], [None], [120, None, -100], [-100, 36, 120, -60, 0], [60, -100],
+]
+
+
+def in_range(st, q, lq, out, window, sinks):
+    """`out` with the exact value in the place of an infinity that stands for what BF16 cannot hold.  A code of 256 or more under a
+    scale of 2^120 is 2^128 and up; the largest BF16 value is 255 2^120, and from 2^128 (1 - 2^-9) on the nearest is infinity.  The
+    weights before that rounding are known to 2^-8 at best: a finite or infinite result is right from 2^128 (1 - 2^-7) on."""
+    out, at = out.double().cpu(), 0
+    for b, n in enumerate(lq):
+        k, v = st.tokens(b)
+        ro = attend(q[at:at + n].cpu(), k, v, st.lens[b] - n, window, sinks)[0]
+        rows = out[at:at + n]
+        beyond = torch.isinf(rows) & (ro.abs() >= 2.0 ** 128 * (1 - 2.0 ** -7)) & (torch.sign(ro) == torch.sign(rows))
+        rows[beyond] = ro[beyond]
+        at += n
+    return out
+
+
+@pytest.mark.parametrize("which", range(len(PAGE_SCALES)))
+@pytest.mark.parametrize("sharp", [0.0, 1.0, 20.0])
+@pytest.mark.parametrize("lens,lq", [([32], [1]), ([64, 300], [1, 5]), ([9000], [9])])
+def test_decode_page_scales_far_apart(which, sharp, lens, lq):
+    """The weights of pages of small values count like any others, and no sum leaves the range of 32 bits.  (Sharp queries: later
+    tokens of small pages outweigh all earlier ones by far more than a sum's reference may lag.)"""
+    st = Store(2, lens, 8, 2, 16, seed=which + 31)
+    for b, n in enumerate(lens):
+        for t in range(-(-n // 16)):
+            e = PAGE_SCALES[which][t % len(PAGE_SCALES[which])]
+            pid = int(st.pt[b, t])
+            st.vs[pid] = 2.0 ** (-100 if e is None else e)
+            if e is None:
+                st.v[pid, :min(16, n - 16 * t)] = 0
+    st.to_gpu()
+    q = queries(st.rng, sum(lq), 8, sharp)
+    for window, sinks in [(0, 0), (150, 20)]:
+        out, lse = st.decode(q, lq, window, sinks)
+        assert bool(torch.isfinite(lse).all())
+        check(st, q, lq, in_range(st, q, lq, out, window, sinks), lse, window, sinks)
+    assert binding.fp2_cache_read_status(st.cache, st.ws)[0] == 0
+
+
+@pytest.mark.parametrize("exponent", [-100, -126, -140, 127])
+def test_decode_a_million_tokens_of_equal_weight(exponent):
+    """All logits are zero: lse = ln n, and out is V whatever its scale."""
+    n, page = 1 << 20, 128
+    cache = binding.Cache(dict(max_seqs=1, num_q_heads=1, num_kv_heads=1, head_dim=D, page_size=page, num_pages=n // page,
+                               max_pages_per_seq=n // page, format=2, softmax_scale=0.0))
+    k, v, ks, vs = cache.new_pages()
+    vs.fill_(2.0 ** exponent)
+    if exponent != -100:
+        v.fill_(0x30)                      # 0.5
+    pt = torch.randperm(n // page, device="cuda").to(torch.int32)[None].contiguous()
+    cu, lk = torch.tensor([0, 1], dtype=torch.int32).cuda(), torch.tensor([n], dtype=torch.int32).cuda()
+    q = torch.randn(1, 1, D, device="cuda").bfloat16()
+    out, lse, ws = torch.full_like(q, math.nan), torch.full((1, 1), math.nan, device="cuda"), cache.new_workspace()
+    binding.fp2_decode(cache, q, k, v, pt, cu, lk, ks, vs, out, lse, ws)
+    # n equal terms summed in 32 bits: by 2^-24 of the sum for every term of a lane's (n / 148 / 2 / 4 / 8 at least), and the joins
+    assert abs(float(lse) - math.log(n)) <= 256 * 2.0 ** -24 + 2.0 ** -20
+    want = 0.0 if exponent == -100 else 2.0 ** (exponent - 1)
+    # the output's rounding, in steps of 2^-133 at the least, beside P's and the sums' as in close()
+    assert bool(((out.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -15) * want + (2.0 ** -134 if want else 0.0)).all())
