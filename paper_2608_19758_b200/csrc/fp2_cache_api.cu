@@ -155,7 +155,7 @@ extern "C" fp2_status fp2_cache_append(const fp2_cache* c, const void* k_new, co
   // 55.2 / 48.6 / 46.6 / 49.9 us, 71.2 / 51.3 / 48.8 / 50.0.
   const int64_t turns = (2ll * c->prm.num_kv_heads * std::max(1, c->prm.page_size / 16) + 7) / 8;
   a.split = (int32_t)std::max<int64_t>(1, std::min<int64_t>(turns, 18 * (c->workers / kDecCtasPerSm) / slots));
-  const int64_t grid = slots * a.split;
+  const int64_t grid = slots * a.split + 1;   // (one for the pages that no slot stands for)
   auto kernel = c->prm.format == FP2_CACHE_BF16 ? cache_append_kernel<FMT_BF16>
                 : c->prm.format == FP2_CACHE_FP8_HEAD ? cache_append_kernel<FMT_FP8_HEAD> : cache_append_kernel<FMT_FP8_PAGE>;
   return launch(kernel, grid, kAppendThreads, 0, stream, a);

@@ -82,49 +82,47 @@ struct AppendArgs {
   CacheGeom g;
 };
 
-template <int FMT>
-__global__ void __launch_bounds__(kAppendThreads, 4)
-cache_append_kernel(AppendArgs A) {
-  constexpr int kRows = 16;           // rows per warp
-  constexpr int kWarps = kAppendThreads / 32;
-  __shared__ uint32_t amax_s[kWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  pdl_trigger();
-  pdl_wait();
-  const int shift = A.g.page_shift, ps = 1 << shift, heads = A.g.num_kv_heads;
-  const int wpi = ps > kRows ? ps / kRows : 1;             // warps per item: 1, 2, 4 or 8
-  const int part = warp % wpi;
-  const long long slot = blockIdx.x / A.split;
+// New tokens of one sequence: rows c0 .. c1 - 1, the sequence L tokens long with them
+struct AppendSeq {
+  int b, c0, c1, L;
+  __device__ __forceinline__ bool fits(const AppendArgs& A) const {
+    return c0 >= 0 && c1 >= c0 && c1 <= A.total_new && L >= c1 - c0 && L <= ((long long)A.g.max_pages << A.g.page_shift);
+  }
+  __device__ __forceinline__ long long first_page(int shift) const { return (L - (c1 - c0)) >> shift; }
+  __device__ __forceinline__ long long last_page(int shift) const { return (L - 1) >> shift; }
+};
 
-  // sequence of the slot: the last one whose first slot is not behind it; 32-way search
+// Sequence of a slot: the last one whose first slot is not behind it; 32-way search by a warp.  (Offsets that fall: any sequence.)
+__device__ __forceinline__ AppendSeq append_find(const AppendArgs& A, long long slot) {
+  const int lane = threadIdx.x & 31, shift = A.g.page_shift;
   int b = 0, n = A.g.num_seqs;
   while (n > 32) {
     const int stride = (n + 31) / 32, i = lane * stride;
     const unsigned bal = __ballot_sync(0xffffffffu, i < n && append_slot0(A.cu[b + min(i, n - 1)], b + i, shift) <= slot);
-    const int skip = max(0, __popc(bal) - 1) * stride;     // (offsets that fall: any sequence)
+    const int skip = max(0, __popc(bal) - 1) * stride;
     b += skip;
     n = min(stride, n - skip);
   }
-  int c0, c1, L;
-  {
-    const int i = b + min(lane, n - 1);
-    const int x0 = A.cu[i], x1 = A.cu[i + 1], l = A.lk[i];
-    const unsigned bal = __ballot_sync(0xffffffffu, lane < n && append_slot0(x0, i, shift) <= slot);
-    const int who = max(0, __popc(bal) - 1);
-    b += who;
-    c0 = __shfl_sync(0xffffffffu, x0, who);
-    c1 = __shfl_sync(0xffffffffu, x1, who);
-    L = __shfl_sync(0xffffffffu, l, who);
-  }
-  if (!(c0 >= 0 && c1 >= c0 && c1 <= A.total_new && L >= c1 - c0 && L <= ((long long)A.g.max_pages << shift))) {
-    if (threadIdx.x == 0) atomicOr(A.status + kCacheStBad, kBadLength);
-    return;
-  }
-  const int first = L - (c1 - c0);
-  const long long page = (first >> shift) + (slot - append_slot0(c0, b, shift));
-  if (c1 == c0 || page < (first >> shift) || page > ((L - 1) >> shift)) return;
+  const int i = b + min(lane, n - 1);
+  const int x0 = A.cu[i], x1 = A.cu[i + 1], l = A.lk[i];
+  const unsigned bal = __ballot_sync(0xffffffffu, lane < n && append_slot0(x0, i, shift) <= slot);
+  const int who = max(0, __popc(bal) - 1);
+  return {b + who, __shfl_sync(0xffffffffu, x0, who), __shfl_sync(0xffffffffu, x1, who), __shfl_sync(0xffffffffu, l, who)};
+}
+
+// A page of a sequence that fits, by CTA `turn0` of `split`
+template <int FMT>
+__device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq& q, long long page, int turn0, int split) {
+  constexpr int kRows = 16;           // rows per warp
+  constexpr int kWarps = kAppendThreads / 32;
+  __shared__ uint32_t amax_s[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int shift = A.g.page_shift, ps = 1 << shift, heads = A.g.num_kv_heads;
+  const int wpi = ps > kRows ? ps / kRows : 1;             // warps per item: 1, 2, 4 or 8
+  const int part = warp % wpi;
+  const int c0 = q.c0, L = q.L, first = L - (q.c1 - c0);
   const int page_tok = (int)page << shift;
-  const int pid = A.page_table[(size_t)b * A.g.max_pages + page];
+  const int pid = A.page_table[(size_t)q.b * A.g.max_pages + page];
   constexpr int esz = FMT == FMT_BF16 ? 2 : 1;
   const int col = lane & 15, half = lane >> 4;
   const int row0 = part * kRows + half;                    // this lane's rows of the page: row0 + 2 i
@@ -137,7 +135,7 @@ cache_append_kernel(AppendArgs A) {
   const long long tok_off = (long long)(c0 + page_tok + row0 - first) * A.stride_bytes + col * 16;
   const bool keeps = first > page_tok;                     // rows in front of the new ones are live
   const int items = 2 * heads, per_turn = kWarps / wpi;    // (the same number of turns for all warps: there is a barrier inside)
-  for (int item0 = (int)(blockIdx.x % A.split) * per_turn; item0 < items; item0 += A.split * per_turn) {
+  for (int item0 = turn0 * per_turn; item0 < items; item0 += split * per_turn) {
     const int item = item0 + warp / wpi;
     const bool active = item < items;
     const bool is_v = item >= heads;
@@ -246,6 +244,52 @@ cache_append_kernel(AppendArgs A) {
       *reinterpret_cast<uint2*>(out + i * row_step) = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);
     }
   }
+}
+
+// Offsets that do not ascend (a sequence that does not fit) shift its neighbours' slots: the pages of sequences that do fit which no
+// slot stands for, all by one CTA.  Apart from the others' code, which has no registers for a loop around a page: prompts 48 us, 55
+// with it.
+template <int FMT>
+__device__ __noinline__ void append_rest(const AppendArgs& A, long long slots) {
+  const int shift = A.g.page_shift;
+  for (int b = 0; b < A.g.num_seqs; ++b) {
+    const AppendSeq q = {b, A.cu[b], A.cu[b + 1], A.lk[b]};
+    if (!q.fits(A)) {
+      if (threadIdx.x == 0) atomicOr(A.status + kCacheStBad, kBadLength);
+      continue;
+    }
+    if (q.c1 == q.c0) continue;
+    for (long long page = q.first_page(shift); page <= q.last_page(shift); ++page) {
+      const long long slot = append_slot0(q.c0, b, shift) + page - q.first_page(shift);
+      if (slot >= slots || append_find(A, slot).b != b) append_page<FMT>(A, q, page, 0, 1);
+    }
+  }
+}
+
+template <int FMT>
+__global__ void __launch_bounds__(kAppendThreads, 4)
+cache_append_kernel(const __grid_constant__ AppendArgs A) {
+  pdl_trigger();
+  pdl_wait();
+  const long long slots = (gridDim.x - 1) / A.split, slot = blockIdx.x / A.split;
+  if (blockIdx.x == gridDim.x - 1) {   // one CTA looks whether the slots are what the others take them for
+    bool ascend = true;
+    for (int i = threadIdx.x; i < A.g.num_seqs; i += kAppendThreads) {
+      const int x0 = A.cu[i], x1 = A.cu[i + 1];
+      ascend &= x0 >= 0 && x1 >= x0 && x1 <= A.total_new;
+    }
+    if (!__syncthreads_and(ascend)) append_rest<FMT>(A, slots);
+    return;
+  }
+  const AppendSeq q = append_find(A, slot);
+  if (!q.fits(A)) {
+    if (threadIdx.x == 0) atomicOr(A.status + kCacheStBad, kBadLength);
+    return;
+  }
+  const int shift = A.g.page_shift;
+  const long long page = q.first_page(shift) + (slot - append_slot0(q.c0, q.b, shift));
+  if (q.c1 == q.c0 || page < q.first_page(shift) || page > q.last_page(shift)) return;
+  append_page<FMT>(A, q, page, (int)(blockIdx.x % A.split), A.split);
 }
 
 // An 8-bit cache as BF16 pages: out = bf16(code * scale), rows of a last page behind the sequence's end zero.  A work item is

@@ -726,3 +726,61 @@ def test_decode_a_million_tokens_of_equal_weight(exponent):
     want = 0.0 if exponent == -100 else 2.0 ** (exponent - 1)
     # the output's rounding, in steps of 2^-133 at the least, beside P's and the sums' as in close()
     assert bool(((out.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -15) * want + (2.0 ** -134 if want else 0.0)).all())
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+@pytest.mark.parametrize("hkv,page", [(2, 16), (1, 128), (3, 8)])
+@pytest.mark.parametrize("cu,lens", [
+    ([0, 1000, 10, 20], [1000, 50, 15]),             # the second one falls; the others fit, the last one's rows are the first one's too
+    ([0, 100, 50, 160], [300, 70, 115]),
+    ([0, 700, 20, 700, 0, 700], [700, 30, 690, 5, 900]),        # more pages than the number of rows asks for
+    ([0, 90, 5000, 30, 160], [100, 6000, 40, 130]),  # past the end of the rows
+    ([0, 90, -7, 30, 160], [100, 20, 40, 135]),
+    ([5, 40, 41, 41, 90, 3], [40, 700, 20, 60, 10]),
+    ([0, 30, 60, 90], [30, 29, 40]),                 # ascending, but a sequence shorter than its new tokens
+])
+def test_append_leaves_out_the_sequence_that_does_not_fit_and_no_other(fmt, hkv, page, cu, lens):
+    """Whatever stands in its neighbours' offsets, a sequence whose own fit is written, and written whole."""
+    total = max(160, max(c for c in cu if c <= 1000))
+    ok = [0 <= a <= b <= total and n >= b - a for a, b, n in zip(cu, cu[1:], lens)]
+    news = [b - a if good else 0 for a, b, good in zip(cu, cu[1:], ok)]
+    had = [n - new if good else 0 for n, new, good in zip(lens, news, ok)]
+    st = Store(fmt, had, hkv, hkv, page, seed=17, capacity=[n if good else 64 for n, good in zip(lens, ok)])
+    x = torch.from_numpy(st.rng.normal(0, 1, (total, 2 * hkv, D))).bfloat16().cuda()
+    rows = torch.tensor([r for a, b, good in zip(cu, cu[1:], ok) if good for r in range(a, b)])
+    want = plain_append(st, x[rows, :hkv], lens, news, "k") + plain_append(st, x[rows, hkv:], lens, news, "v")
+    binding.fp2_cache_append(st.cache, x[:, :hkv], x[:, hkv:], st.dpt, torch.tensor(cu, dtype=torch.int32).cuda(),
+                             torch.tensor(lens, dtype=torch.int32).cuda(), st.dk, st.dv, st.dks, st.dvs, st.ws)
+    for got, ref in zip((st.dk, st.dks, st.dv, st.dvs), want):
+        assert same(got, ref)
+    code, words = binding.fp2_cache_read_status(st.cache, st.ws, raise_on_error=False)
+    assert code == 1 and words[2] == 4
+
+
+@pytest.mark.parametrize("fmt", [0, 2])
+def test_more_sequences_than_one_search_step_tells_apart(fmt):
+    """1500 sequences: appending, reading back, decoding (a search of 32 x 32 sequences, and scans of 128, take more than one round)."""
+    rng = np.random.default_rng(51)
+    news = [int(x) for x in rng.integers(0, 4, 1500)]
+    had = [int(x) for x in rng.integers(0, 40, 1500)]
+    lens = [a + n for a, n in zip(had, news)]
+    st = Store(fmt, had, 2, 1, 16, seed=51, capacity=lens)
+    x = torch.from_numpy(rng.normal(0, 1, (sum(news), 2, D))).bfloat16().cuda()
+    want = plain_append(st, x[:, :1], lens, news, "k") + plain_append(st, x[:, 1:], lens, news, "v")
+    run_append(st, x[:, :1], x[:, 1:], lens, news)
+    for got, ref in zip((st.dk, st.dks, st.dv, st.dvs), want):
+        assert same(got, ref)
+    q = queries(rng, sum(news), 2)
+    out, lse = st.decode(q, news, lens=lens)
+    check(st, q, news, out, lse, 0, 0, lens=lens)
+    if fmt:
+        k, v = (torch.full((st.pool, 16, 1, D), 9.0, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+        binding.fp2_cache_expand(st.cache, st.dk, st.dv, st.dpt, torch.tensor(lens, dtype=torch.int32).cuda(), st.dks, st.dvs, k, v,
+                                 st.dpt, st.ws)
+        for o, i in ((k, 0), (v, 1)):
+            got = o.cpu()
+            for b, n in enumerate(lens):
+                ref = torch.zeros(-(-n // 16) * 16, 1, D, dtype=torch.float64)
+                ref[:n] = st.tokens(b, n)[i]
+                assert torch.equal(got[[int(p) for p in st.pt[b, :-(-n // 16)]]].view(-1, 1, D).double(), ref)
+    assert binding.fp2_cache_read_status(st.cache, st.ws)[0] == 0
