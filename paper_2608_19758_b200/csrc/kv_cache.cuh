@@ -82,6 +82,18 @@ struct AppendArgs {
   CacheGeom g;
 };
 
+// a / s in 32 bits rounded to odd (towards zero, the last bit set where something was cut off): rounded again to fewer bits, to
+// nearest, it gives what the quotient itself would.  Where the remainder, exact in 32 bits, could fall below their range both are
+// brought up; a NaN or infinity stays.  (A call: seldom needed, and in line it took registers from the common path, 45.0 against 44.5 us
+// for 41392 tokens with a scale per head.)
+__device__ __noinline__ float div_to_odd(float a, float s) {
+  const float up = s < 0x1p-60f ? 0x1p64f : 1.f;
+  a *= up;
+  s *= up;
+  const float q = __fdiv_rz(a, s), rem = fmaf(-q, s, a);
+  return __uint_as_float(__float_as_uint(q) | (rem < 0.f || rem > 0.f ? 1u : 0u));
+}
+
 // New tokens of one sequence: rows c0 .. c1 - 1, the sequence L tokens long with them
 struct AppendSeq {
   int b, c0, c1, L;
@@ -214,7 +226,7 @@ __device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq
       if (part == 0 && lane == 0) *where = scale;
     }
     // A power of two divides exactly.  Another scale (a caller's): the quotient lies between the products with a reciprocal rounded
-    // down and one rounded up, 2^-21 each way; where both round to the same e4m3 value so does it, and else it is divided.
+    // down and one rounded up, 2^-21 each way; where both round to the same e4m3 value so does it, and else it is divided, once rounded.
     const bool pow2 = (__float_as_uint(scale) & 0x7fffffu) == 0u, usual = scale >= 0x1p-100f && scale <= 0x1p126f;
     const float inv = 1.0f / scale, inv_lo = inv * (1.f - 0x1p-21f), inv_hi = inv * (1.f + 0x1p-21f);
     auto quantise = [&](uint32_t w, float f) { return pack_e4m3x2(bf16_lo(w) * f, bf16_hi(w) * f); };
@@ -238,7 +250,7 @@ __device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq
         }
         if (differ) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[k] = pack_e4m3x2(__fdiv_rn(bf16_lo(w[k]), scale), __fdiv_rn(bf16_hi(w[k]), scale));
+          for (int k = 0; k < 4; ++k) o[k] = pack_e4m3x2(div_to_odd(bf16_lo(w[k]), scale), div_to_odd(bf16_hi(w[k]), scale));
         }
       }
       *reinterpret_cast<uint2*>(out + i * row_step) = make_uint2(o[0] | o[1] << 16, o[2] | o[3] << 16);

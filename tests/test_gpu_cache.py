@@ -784,3 +784,30 @@ def test_more_sequences_than_one_search_step_tells_apart(fmt):
                 ref[:n] = st.tokens(b, n)[i]
                 assert torch.equal(got[[int(p) for p in st.pt[b, :-(-n // 16)]]].view(-1, 1, D).double(), ref)
     assert binding.fp2_cache_read_status(st.cache, st.ws)[0] == 0
+
+
+def test_append_rounds_the_quotient_once():
+    """Scales of the caller's that put quotients next to the middle between two e4m3 values: the code nearest to the exact quotient.
+    (|x| against middle times scale: 29 bits, exact in 64.)"""
+    rng = np.random.default_rng(4)
+    hkv, n = 64, 16
+    pos = e4m3_values()[:127].numpy()
+    x = torch.from_numpy(rng.integers(128, 256, (n, hkv, D)) / 128 * np.where(rng.random((n, hkv, D)) < 0.5, -1, 1)).bfloat16()
+    i = rng.integers(20, 100, hkv)
+    middle = (pos[i] + pos[i + 1]) / 2
+    s = (np.abs(x[0, :, 0].double().numpy()) / middle).astype(np.float32)      # token 0, dim 0 of every head is next to a tie
+    s = np.nextafter(s, np.where(np.arange(hkv) % 3 == 0, 0, np.where(np.arange(hkv) % 3 == 1, np.inf, s)).astype(np.float32)).astype(np.float32)
+    st = Store(1, [0], hkv, hkv, 16, capacity=[n])
+    st.dks, st.dvs = torch.from_numpy(s).cuda(), torch.from_numpy(s).cuda()
+    run_append(st, x.cuda(), x.cuda(), [n], [n])
+    xd, sd = x.double().numpy(), s.astype(np.float64)[None, :, None]
+    a = np.minimum(np.abs(xd), 448 * sd)
+    # the last value whose product with the scale is not above |x|, found on the quotient and corrected by comparing products
+    lo = np.clip(np.searchsorted(pos, a / sd, side="right") - 1, 0, 125)
+    lo = np.where(pos[lo] * sd > a, lo - 1, lo)
+    lo = np.where(pos[lo + 1] * sd <= a, np.minimum(lo + 1, 125), lo)
+    border = (pos[lo] + pos[lo + 1]) / 2 * sd
+    code = np.where((a > border) | ((a == border) & (lo % 2 == 1)), lo + 1, lo)
+    code = torch.from_numpy((code + 128 * np.signbit(xd)).astype(np.uint8))
+    got = st.dk[int(st.pt[0, 0])].cpu()
+    assert torch.equal(got, code) and torch.equal(st.dv[int(st.pt[0, 0])].cpu(), code)
