@@ -306,8 +306,9 @@ cache_append_kernel(const __grid_constant__ AppendArgs A) {
 
 // An 8-bit cache as BF16 pages: out = bf16(code * scale), rows of a last page behind the sequence's end zero.  A work item is
 // one group of up to 16 rows of a page, all heads, K or V: consecutive 16-byte pieces to consecutive threads.  Bound by memory:
-// one byte read and two written per element.  90816 tokens, 8 heads, 16 a page: 91.3 us, 6.1 TB/s, 0.93 of the copy rate (stores of
-// 16 bytes, half a sector each, 102; one / two pieces of a thread on their way 107.7 / 98.6).
+// one byte read and two written per element.  90816 tokens, 8 heads, 16 a page: 94.5 us, 5.9 TB/s, 0.90 of the copy rate (without the
+// question of how a product rounds 92.0; stores of 16 bytes, half a sector each, 102; one / two pieces of a thread on their way 107.7 /
+// 98.6).  Three CTAs to an SM: two / four 102.1 / 100.5.
 constexpr int kExpandThreads = 256;
 constexpr int kExpandBatch = 4;       // pieces of a thread on their way at a time
 
@@ -316,6 +317,29 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t (&r)[8]) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
                "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
+}
+
+// code * scale has up to 28 bits.  Rounded to 32 bits and then to BF16 it may end on the wrong side of the middle between two BF16
+// values, where the first rounding brings it there.  Not so with a scale of 20 bits or less (the product is exact; the writer's powers
+// of two), and with few others: it takes one of the eight significands of a code next to a middle (looked at where no product leaves
+// the range).
+__device__ __forceinline__ bool exact_products(float s) { return (__float_as_uint(s) & 15u) == 0u && s >= 0x1p-100f; }
+__device__ __forceinline__ bool rounds_twice(float s) {
+  bool bad = !(s >= 0x1p-100f);
+#pragma unroll
+  for (int c = 8; c < 16; ++c) bad |= (__float_as_uint(s * (c * 0x1p-7f)) & 0xffffu) == 0x8000u;
+  return bad && !exact_products(s);
+}
+// Then the product is rounded to odd (see div_to_odd; up: 2^64 where what was cut off could fall below the range of 32 bits), which
+// leaves the one rounding to BF16.  Two codes; a call, to leave its registers to the common path.
+__device__ __forceinline__ float mul_to_odd(float a, float s, float up) {
+  const float p = __fmul_rz(a, s), cut = fmaf(a, s * up, -(p * up));
+  return __uint_as_float(__float_as_uint(p) | (cut < 0.f || cut > 0.f ? 1u : 0u));
+}
+__device__ __noinline__ uint32_t widen_rounding_once(uint32_t codes, float s) {
+  const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(codes & 0xffffu));
+  const float up = s < 0x1p-60f ? 0x1p64f : 1.f;
+  return pack_bf16x2(mul_to_odd(a.x, s, up), mul_to_odd(a.y, s, up));
 }
 
 struct ExpandArgs {
@@ -329,7 +353,7 @@ struct ExpandArgs {
 };
 
 template <int FMT>
-__global__ void __launch_bounds__(kExpandThreads)
+__global__ void __launch_bounds__(kExpandThreads, 3)
 cache_expand_kernel(ExpandArgs A) {
   const int lane = threadIdx.x & 31;
   pdl_trigger();
@@ -338,6 +362,11 @@ cache_expand_kernel(ExpandArgs A) {
   const int gshift = shift < 4 ? shift : 4;               // rows of a group
   const int groups = 1 << (shift - gshift);               // per page
   const int pieces = (heads * 8) << gshift;               // 16-byte pieces of a group
+  bool careful = false;
+  if constexpr (FMT == FMT_FP8_HEAD) {                     // (a scale per page is looked at where it is used)
+    for (int h = threadIdx.x; h < 2 * heads; h += kExpandThreads) careful |= rounds_twice(h < heads ? A.k_scale[h] : A.v_scale[h - heads]);
+    careful = __syncthreads_or(careful);
+  }
   // items: (sequence, group of rows), K and V of it next to each other
   long long item = blockIdx.x;
   long long base = 0;                                      // items in front of the 32 sequences looked at
@@ -382,7 +411,24 @@ cache_expand_kernel(ExpandArgs A) {
           const int row = hr / heads;
           const bool in = c < pieces && row < left;
           v[k] = in ? *reinterpret_cast<const uint4*>(src + (size_t)c * 16) : make_uint4(0, 0, 0, 0);
-          s[k] = in ? scale[hr - row * heads] : 0.f;
+          s[k] = in ? scale[hr - row * heads] : 1.f;
+        }
+        bool once = !careful;                              // the product's rounding to 32 bits loses nothing
+        if constexpr (FMT == FMT_FP8_PAGE) {
+#pragma unroll
+          for (int k = 0; k < kExpandBatch; ++k) once &= exact_products(s[k]);
+        }
+        if (!once) {
+#pragma unroll
+          for (int k = 0; k < kExpandBatch; ++k)
+            if (c0 + k * kExpandThreads < pieces) {
+              const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+              uint32_t o[8];
+#pragma unroll
+              for (int j = 0; j < 8; ++j) o[j] = widen_rounding_once(w[j / 2] >> (j & 1) * 16, s[k]);
+              st_global_32(dst + (size_t)(c0 + k * kExpandThreads) * 32, o);
+            }
+          continue;
         }
 #pragma unroll
         for (int k = 0; k < kExpandBatch; ++k) {

@@ -811,3 +811,45 @@ def test_append_rounds_the_quotient_once():
     code = torch.from_numpy((code + 128 * np.signbit(xd)).astype(np.uint8))
     got = st.dk[int(st.pt[0, 0])].cpu()
     assert torch.equal(got, code) and torch.equal(st.dv[int(st.pt[0, 0])].cpu(), code)
+
+
+def nearest_bf16(x):
+    """64-bit numbers to the nearest of eight significant bits, ties to even (normal numbers), as BF16."""
+    m, e = np.frexp(x)
+    return torch.from_numpy(np.ldexp(np.round(m * 256) / 256, e)).bfloat16()
+
+
+def scales_at_ties():
+    """fp32 scales under which a code lies next to the middle between two BF16 values: 1.625 * 1.5432693 among them."""
+    rng = np.random.default_rng(3)
+    code = np.arange(1, 2, 0.125)[rng.integers(0, 8, 500)]
+    middle = (rng.integers(128, 256, 500) + 0.5) / 128
+    s = (middle / code).astype(np.float32)
+    s[0] = 1.5432693
+    return np.nextafter(s, np.where(rng.random(500) < 0.5, 0, 9).astype(np.float32)).astype(np.float32)
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+def test_expand_rounds_once(fmt):
+    """All codes under scales that put some of them next to a tie: the exact product (28 bits) rounded to BF16, and not to 32 bits on
+    the way."""
+    scales = torch.from_numpy(np.concatenate([scales_at_ties(), [np.float32(1.5432693)], np.float32(2.0) ** np.arange(-100, 100, 17)]).astype(np.float32))
+    n = len(scales)
+    hkv, pages = (n, 1) if fmt == 1 else (1, n)
+    cache = binding.Cache(dict(max_seqs=1, num_q_heads=hkv, num_kv_heads=hkv, head_dim=D, page_size=8, num_pages=pages,
+                               max_pages_per_seq=pages, format=fmt, softmax_scale=0.0))
+    codes = torch.arange(256, dtype=torch.uint8).view(2, 1, D)          # tokens 0 and 1 of every page
+    k = torch.zeros(pages, 8, hkv, D, dtype=torch.uint8)
+    k[:, :2] = codes
+    s = scales.cuda() if fmt == 1 else scales.cuda()[:, None].contiguous()
+    pt = torch.arange(pages, dtype=torch.int32).cuda()[None].contiguous()
+    out, o2 = (torch.zeros(pages, 8, hkv, D, dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    binding.fp2_cache_expand(cache, k.cuda(), k.cuda(), pt, torch.tensor([8 * pages], dtype=torch.int32).cuda(), s, s, out, o2, pt,
+                             cache.new_workspace())
+    exact = codes.view(E4M3).double()[:, :, None, :] * scales.double()[None, None, :, None]       # [2, 1, n, D]
+    finite = ~torch.isnan(exact)
+    ref = nearest_bf16(torch.nan_to_num(exact).numpy())
+    for got in (out, o2):
+        got = got[:, :2].cpu()
+        got = got.permute(1, 0, 2, 3) if fmt == 1 else got.permute(1, 2, 0, 3)
+        assert bool(torch.isnan(got[~finite]).all()) and torch.equal(got[finite], ref[finite])
