@@ -491,7 +491,7 @@ decode_kernel(DecodeArgs A) {
         const float f = __uint_as_float((uint32_t)(e + 127) << 23), back = __uint_as_float((uint32_t)(127 - e) << 23);
         mul *= back;
         if constexpr (FMT == FMT_FP8_HEAD) mul *= k_scale;
-        mul = fmaxf(mul, 1e-37f);        // (a hidden logit of -inf times zero would be NaN)
+        if constexpr (!OWN_E) mul = fmaxf(mul, 1e-37f);   // (a hidden logit of -inf times zero would be NaN; pages' scales come first)
 #pragma unroll
         for (int s = 0; s < 8; ++s)
 #pragma unroll

@@ -853,3 +853,15 @@ def test_expand_rounds_once(fmt):
         got = got[:, :2].cpu()
         got = got.permute(1, 0, 2, 3) if fmt == 1 else got.permute(1, 2, 0, 3)
         assert bool(torch.isnan(got[~finite]).all()) and torch.equal(got[finite], ref[finite])
+
+
+@pytest.mark.parametrize("fmt", [1, 2])
+@pytest.mark.parametrize("key,query", [(118, -124), (100, -100), (-100, 100), (-118, 110)])
+def test_decode_small_queries_on_large_keys(fmt, key, query):
+    """Logits of ordinary size from factors at the ends of their range."""
+    st = Store(fmt, [200, 40], 8, 2, 16, seed=41)
+    st.ks.fill_(2.0 ** (key - 6))          # codes are about 60
+    st.to_gpu()
+    q = torch.from_numpy(st.rng.normal(0, 1.5, (6, 8, D)) * 2.0 ** query).bfloat16().cuda()
+    out, lse = st.decode(q, [5, 1])
+    check(st, q, [5, 1], out, lse, 0, 0)
