@@ -277,7 +277,8 @@ fp2_status fp2_selftest_bounded_wait(fp2_plan* plan, void* workspace, fp2_stream
  *
  * Lengths on the device that do not fit -- offsets that fall or pass the number of rows, more tokens than max_pages_per_seq
  * pages hold -- make the calls leave that sequence out; a page id outside [0, num_pages) leaves out the tokens of that page.
- * Both are recorded in the workspace's status block (fp2_cache_read_status). */
+ * Both are recorded in the workspace's status block (fp2_cache_read_status).
+ * A call without sequences (num_seqs 0) does nothing; page table, lengths and offsets may be NULL then. */
 typedef enum { FP2_CACHE_BF16 = 0, FP2_CACHE_FP8_HEAD = 1, FP2_CACHE_FP8_PAGE = 2 } fp2_cache_format;
 
 typedef struct fp2_cache fp2_cache; /* opaque */

@@ -97,10 +97,13 @@ static CacheGeom geom(const fp2_cache* c, int num_seqs) {
   return CacheGeom{c->prm.num_kv_heads, c->page_shift, c->prm.num_pages, c->prm.max_pages_per_seq, num_seqs};
 }
 
+// What all calls take.  No sequences: nothing is read, and arrays of them (page table, lengths, offsets) may be NULL, as those of
+// empty tensors are.
 static fp2_status check_cache(const fp2_cache* c, const void* k, const void* v, const void* pt, const void* lk, const float* ks,
                               const float* vs, const void* ws, int32_t num_seqs) {
-  if (!c || !on(k, 16) || !on(v, 16) || !pt || !lk || !on(ws, 1024)) return FP2_ERR_INVALID_ARG;
+  if (!c || !on(k, 16) || !on(v, 16) || !on(ws, 1024)) return FP2_ERR_INVALID_ARG;
   if (c->prm.format != FP2_CACHE_BF16 && (!ks || !vs)) return FP2_ERR_INVALID_ARG;
+  if (num_seqs != 0 && (!pt || !lk)) return FP2_ERR_INVALID_ARG;
   return num_seqs < 0 || num_seqs > c->prm.max_seqs ? FP2_ERR_INVALID_ARG : FP2_OK;
 }
 
@@ -135,7 +138,7 @@ extern "C" fp2_status fp2_cache_append(const fp2_cache* c, const void* k_new, co
                                        fp2_stream stream) {
   fp2_status s = check_cache(c, k, v, page_table, lk, ks, vs, workspace, num_seqs);
   if (s != FP2_OK) return s;
-  if (!cu || total_new < 0) return FP2_ERR_INVALID_ARG;
+  if ((!cu && num_seqs > 0) || total_new < 0) return FP2_ERR_INVALID_ARG;
   if (num_seqs == 0 || total_new == 0) return FP2_OK;
   if (!on(k_new, 16) || !on(v_new, 16)) return FP2_ERR_INVALID_ARG;
   if (new_stride < (int64_t)c->prm.num_kv_heads * kHeadDim || new_stride % 8 != 0) return FP2_ERR_INVALID_ARG;
@@ -168,9 +171,10 @@ extern "C" fp2_status fp2_cache_expand(const fp2_cache* c, const void* k, const 
   if (c && c->prm.format == FP2_CACHE_BF16) return FP2_ERR_UNSUPPORTED;   // it is BF16 pages already
   fp2_status s = check_cache(c, k, v, page_table, lk, ks, vs, workspace, num_seqs);
   if (s != FP2_OK) return s;
-  if (!out_page_table || out_num_pages < 0) return FP2_ERR_INVALID_ARG;
+  if (out_num_pages < 0) return FP2_ERR_INVALID_ARG;
   if (num_seqs == 0) return FP2_OK;
-  if (!on(k_out, 32) || !on(v_out, 32)) return FP2_ERR_INVALID_ARG;
+  if (!out_page_table) return FP2_ERR_INVALID_ARG;
+  if (out_num_pages > 0 && (!on(k_out, 32) || !on(v_out, 32))) return FP2_ERR_INVALID_ARG;
   if ((s = check_device(c)) != FP2_OK) return s;
   ExpandArgs a;
   a.k_cache = (const uint8_t*)k; a.v_cache = (const uint8_t*)v;
@@ -201,7 +205,7 @@ extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_st
                                  void* out, float* lse, void* workspace, fp2_stream stream) {
   fp2_status s = check_cache(c, k, v, page_table, lk, ks, vs, workspace, num_seqs);
   if (s != FP2_OK) return s;
-  if (!cu || total_q < 0 || window_tokens < 0 || sink_tokens < 0) return FP2_ERR_INVALID_ARG;
+  if ((!cu && num_seqs > 0) || total_q < 0 || window_tokens < 0 || sink_tokens < 0) return FP2_ERR_INVALID_ARG;
   if (num_seqs == 0 || total_q == 0) return FP2_OK;
   if (!on(q, 16) || !on(out, 16)) return FP2_ERR_INVALID_ARG;
   if (q_stride < (int64_t)c->prm.num_q_heads * kHeadDim || q_stride % 8 != 0) return FP2_ERR_INVALID_ARG;

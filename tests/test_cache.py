@@ -1,5 +1,6 @@
 """The paged KV cache on the host: what its calls refuse, before anything is launched."""
 import ctypes as C
+import types
 
 import pytest
 import torch
@@ -160,3 +161,25 @@ def test_cache_create_at_its_limits(kw, code):
     with pytest.raises(binding.Fp2Error) as e:
         binding.Cache(cache_params(**kw))
     assert e.value.code == code
+
+
+@pytest.mark.parametrize("fmt", [0, 1, 2])
+def test_an_empty_batch_is_nothing_to_do(fmt):
+    """No sequences, as an engine's tensors say it: these have no address."""
+    dev = "cuda" if torch.cuda.is_available() else "cpu"
+    cache = binding.Cache(cache_params(format=fmt))
+    k, v, ks, vs = cache.new_pages(dev)
+    ws, pt = cache.new_workspace(dev), torch.zeros(0, 32, dtype=torch.int32, device=dev)
+    lk, cu = torch.zeros(0, dtype=torch.int32, device=dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    assert pt.data_ptr() == 0 and lk.data_ptr() == 0
+    stream = types.SimpleNamespace(cuda_stream=0)      # (asking torch for one takes a device)
+    q, new = torch.zeros(0, 8, 128, dtype=torch.bfloat16, device=dev), torch.zeros(0, 2, 128, dtype=torch.bfloat16, device=dev)
+    binding.fp2_cache_append(cache, new, new, pt, cu, lk, k, v, ks, vs, ws, stream=stream)
+    binding.fp2_decode(cache, q, k, v, pt, cu, lk, ks, vs, q.clone(), torch.zeros(8, 0, device=dev), ws, stream=stream)
+    if fmt:
+        out = torch.zeros(0, 16, 2, 128, dtype=torch.bfloat16, device=dev)
+        binding.fp2_cache_expand(cache, k, v, pt, lk, ks, vs, out, out.clone(), pt, ws, stream=stream)
+    lib = binding.load()
+    assert lib.fp2_cache_append(cache.handle, 4096, 4096, 256, None, None, None, 1, 1, 4096, 4096, 4096, 4096, 4096, None) == 1
+    assert lib.fp2_decode(cache.handle, 4096, 1024, 4096, 4096, None, None, None, 1, 1, 4096, 4096, 0, 0, 4096, None, 4096, None) == 1
+    cache.close()
