@@ -170,6 +170,12 @@ class Plan:
         a, b, c = C.c_int64(), C.c_int64(), C.c_int64()
         _check(lib.fp2_plan_sizes(h, C.byref(a), C.byref(b), C.byref(c)), "fp2_plan_sizes")
         self.num_segments, self.idx_capacity, self.workspace_bytes = a.value, b.value, c.value
+        self._device = torch.cuda.current_device() if torch.cuda.is_available() else -1
+        p = self.params
+        self._fp8 = p.dtype != 0
+        self._kinds = _E4M3 if self._fp8 else _BF16
+        self._q_size, self._pool_size = p.total_q * p.num_q_heads * 128, p.num_pages * p.page_size * p.num_kv_heads * 128
+        self._pt_shape, self._lse_shape = (p.num_seqs, p.max_pages_per_seq), (p.num_q_heads, p.total_q)
 
     def segment(self, seg: int) -> dict:
         out = (C.c_int32 * 10)()
@@ -249,10 +255,30 @@ def fp2_dense_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q,
 def fp2_window_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale, v_scale,
                        window_tokens: int, sink_tokens: int, out, lse, workspace, stream=None):
     """Causal attention with a sliding window of `window_tokens` and the first `sink_tokens` tokens always visible."""
+    where, dev, kinds = "fp2_window_prefill", plan._device, plan._kinds
+    if not (q.dtype in kinds and q.numel() >= plan._q_size and q.get_device() == dev and q.is_contiguous() and
+            k_cache.dtype in kinds and k_cache.numel() >= plan._pool_size and k_cache.get_device() == dev and k_cache.is_contiguous() and
+            v_cache.dtype in kinds and v_cache.numel() >= plan._pool_size and v_cache.get_device() == dev and v_cache.is_contiguous() and
+            out.dtype is torch.bfloat16 and out.numel() >= plan._q_size and out.get_device() == dev and out.is_contiguous()):
+        _room(where, dev, q, kinds, plan._q_size)
+        _room(where, dev, k_cache, kinds, plan._pool_size)
+        _room(where, dev, v_cache, kinds, plan._pool_size)
+        _room(where, dev, out, _BF16, plan._q_size)
+    if not (page_table.dtype is torch.int32 and page_table.shape == plan._pt_shape and page_table.get_device() == dev and
+            page_table.is_contiguous()):
+        _want(where, dev, page_table, _I32, plan._pt_shape)
+    if lse is not None and not (lse.dtype is torch.float32 and lse.shape == plan._lse_shape and lse.get_device() == dev and
+                                lse.is_contiguous()):
+        _want(where, dev, lse, _F32, plan._lse_shape)
+    if plan._fp8:
+        _room(where, dev, q_scale, _F32, plan.params.num_q_heads)
+        _room(where, dev, k_scale, _F32, plan.params.num_kv_heads)
+        _room(where, dev, v_scale, _F32, plan.params.num_kv_heads)
+    if workspace.nbytes < plan.workspace_bytes or workspace.get_device() != dev:
+        raise Fp2Error(1, f"{where}: workspace too small or not on device {dev}")
     _check(load().fp2_window_prefill(plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
                                      _ptr(cu_seqlens_q), _ptr(seqlens_k), _ptr(q_scale), _ptr(k_scale), _ptr(v_scale),
-                                     window_tokens, sink_tokens, _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)),
-           "fp2_window_prefill")
+                                     window_tokens, sink_tokens, _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)), where)
 
 
 def fp2_dense_prefill_static(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale,
@@ -381,6 +407,13 @@ def _want(where, dev, t, dtypes, shape):
     if t is None or t.dtype not in dtypes or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
         got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}"
         raise Fp2Error(1, f"{where}: wanted contiguous {dtypes[0]} {shape} on device {dev}, got {got}")
+
+
+def _room(where, dev, t, dtypes, size):
+    """As _want, for a tensor that may have more elements behind those that the call takes."""
+    if t is None or t.dtype not in dtypes or t.numel() < size or t.get_device() != dev or not t.is_contiguous():
+        got = "None" if t is None else f"{t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}"
+        raise Fp2Error(1, f"{where}: wanted contiguous {dtypes[0]}, {size} elements on device {dev}, got {got}")
 
 
 def _rows(where, dev, t, heads):

@@ -183,3 +183,39 @@ def test_an_empty_batch_is_nothing_to_do(fmt):
     assert lib.fp2_cache_append(cache.handle, 4096, 4096, 256, None, None, None, 1, 1, 4096, 4096, 4096, 4096, 4096, None) == 1
     assert lib.fp2_decode(cache.handle, 4096, 1024, 4096, 4096, None, None, None, 1, 1, 4096, 4096, 0, 0, 4096, None, 4096, None) == 1
     cache.close()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_window_prefill_refuses_tensors_that_are_not_what_the_address_is_taken_for(fp8):
+    """Queries that are a slice of a fused projection, other types, fewer elements, other row lengths; what has more elements behind
+    those of the call goes through (to the lack of a device)."""
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    prm = dict(num_seqs=2, total_q=300, num_q_heads=8, num_kv_heads=2, head_dim=128, block_size=128, tile_rows=128, page_size=16,
+               num_pages=64, max_pages_per_seq=32, sink_tokens=256, window_tokens=512, use_correction=1, alpha=0.1,
+               softmax_scale=0.0, dtype=1 if fp8 else 0)
+    plan = binding.Plan(prm, [0, 200, 300], [400, 100])
+    kind = torch.uint8 if fp8 else torch.bfloat16
+    q, k = torch.zeros(300, 8, 128, dtype=kind), torch.zeros(64, 16, 2, 128, dtype=kind)
+    out, lse, pt = torch.zeros(300, 8, 128, dtype=torch.bfloat16), torch.zeros(8, 300), torch.zeros(2, 32, dtype=torch.int32)
+    scale = torch.ones(8) if fp8 else None
+    good = dict(q=q, k_cache=k, v_cache=k.clone(), page_table=pt, cu_seqlens_q=torch.tensor([0, 200, 300], dtype=torch.int32),
+                seqlens_k=torch.tensor([400, 100], dtype=torch.int32), q_scale=scale, k_scale=scale, v_scale=scale, window_tokens=16,
+                sink_tokens=0, out=out, lse=lse, workspace=plan.new_workspace("cpu"), stream=types.SimpleNamespace(cuda_stream=0))
+    bad = [("q", torch.zeros(300, 12, 128, dtype=kind)[:, :8]), ("q", q.float()), ("q", q[:299]), ("q", torch.zeros(8, 300, 128, dtype=kind).transpose(0, 1)),
+           ("k_cache", k[:63]), ("v_cache", k.to(torch.int32)), ("v_cache", torch.zeros(64, 16, 4, 128, dtype=kind)[:, :, ::2]),
+           ("page_table", pt.long()), ("page_table", torch.zeros(2, 40, dtype=torch.int32)), ("page_table", torch.zeros(2, 40, dtype=torch.int32)[:, :32]),
+           ("out", torch.zeros(300, 16, 128, dtype=torch.bfloat16)[:, :8]), ("out", out.float()), ("out", out[1:]), ("lse", lse.T), ("lse", torch.zeros(8, 400)),
+           ("lse", lse.double()), ("workspace", good["workspace"][:64])]
+    if fp8:
+        bad += [("q_scale", None), ("q_scale", torch.ones(7)), ("k_scale", torch.ones(2).double()), ("v_scale", torch.ones(4)[::2])]
+    for name, value in bad:
+        with pytest.raises(binding.Fp2Error) as e:
+            binding.fp2_window_prefill(plan, **{**good, name: value})
+        assert e.value.code == 1, (name, value.shape if value is not None else None)
+    more = dict(q=torch.zeros(400, 8, 128, dtype=kind), out=torch.zeros(400, 8, 128, dtype=torch.bfloat16), k_cache=torch.zeros(70, 16, 2, 128, dtype=kind))
+    for kw in ({}, more, dict(lse=None), dict(k_cache=k.view(-1, 2, 128))):
+        with pytest.raises(binding.Fp2Error) as e:
+            binding.fp2_window_prefill(plan, **{**good, **kw})
+        assert e.value.code == 4
+    plan.close()
