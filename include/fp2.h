@@ -157,7 +157,7 @@ fp2_status fp2_dense_prefill(fp2_plan* plan, const void* q, const void* k_cache,
  * Entries of pages that no query sees -- wholly in front of all windows and behind the sinks -- may be anything (pages that were
  * given back).  What stands in places that no query of a 128-row tile sees, rows of a last page behind the sequence's end among
  * them, never matters; V of a token that some query of a tile sees must be finite for the others.  Arguments and results otherwise
- * as fp2_dense_prefill.  Two kernels on `stream`. */
+ * as fp2_dense_prefill.  Two kernels on `stream`; none, whatever the pointers, for a plan without new tokens. */
 fp2_status fp2_window_prefill(fp2_plan* plan, const void* q, const void* k_cache, const void* v_cache,
                               const int32_t* page_table, const int32_t* cu_seqlens_q, const int32_t* seqlens_k,
                               const float* q_scale, const float* k_scale, const float* v_scale, int32_t window_tokens,

@@ -732,13 +732,17 @@ extern "C" fp2_status fp2_window_prefill(fp2_plan* pl, const void* q, const void
                                          const int32_t* cu, const int32_t* lk, const float* qs, const float* ks, const float* vs,
                                          int32_t window_tokens, int32_t sink_tokens, void* out, float* lse, void* workspace,
                                          fp2_stream stream) {
-  if (window_tokens < 1 || sink_tokens < 0 || !out_ok(pl, out)) return FP2_ERR_INVALID_ARG;
+  if (!pl || window_tokens < 1 || sink_tokens < 0) return FP2_ERR_INVALID_ARG;
+  if (pl->nseg == 0) {   // no new tokens: nothing to do, and q and out, empty, have no address
+    pl->last_launches = 0;
+    return FP2_OK;
+  }
+  if (!out_ok(pl, out)) return FP2_ERR_INVALID_ARG;
   fp2_status s = check_common(pl, q, k, v, pt, cu, lk, qs, ks, vs, workspace);
   if (s != FP2_OK) return s;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace);
   pl->last_launches = 0;
-  if (pl->nseg == 0) return FP2_OK;
   const int most = kMaxBlocks * kBlock;   // (no position is further away; the kernel's sums stay in 32 bits)
   const int window = std::min(window_tokens, most), sinks = std::min(sink_tokens, most);
   // iterations of a segment: the blocks of the first row's window and of the rows behind it, and of the sinks

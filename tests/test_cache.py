@@ -219,3 +219,18 @@ def test_window_prefill_refuses_tensors_that_are_not_what_the_address_is_taken_f
             binding.fp2_window_prefill(plan, **{**good, **kw})
         assert e.value.code == 4
     plan.close()
+
+
+def test_window_prefill_without_new_tokens_is_nothing_to_do():
+    dev = "cuda" if torch.cuda.is_available() else "cpu"
+    prm = dict(num_seqs=2, total_q=0, num_q_heads=8, num_kv_heads=2, head_dim=128, block_size=128, tile_rows=128, page_size=16,
+               num_pages=64, max_pages_per_seq=32, sink_tokens=256, window_tokens=512, use_correction=1, alpha=0.1,
+               softmax_scale=0.0, dtype=0)
+    plan = binding.Plan(prm, [0, 0, 0], [400, 0])
+    q, k = torch.zeros(0, 8, 128, dtype=torch.bfloat16, device=dev), torch.zeros(64, 16, 2, 128, dtype=torch.bfloat16, device=dev)
+    ints = lambda *shape: torch.zeros(*shape, dtype=torch.int32, device=dev)
+    binding.fp2_window_prefill(plan, q, k, k.clone(), ints(2, 32), ints(3), ints(2), None, None, None, 16, 0, q.clone(),
+                               torch.zeros(8, 0, device=dev), plan.new_workspace(dev), stream=types.SimpleNamespace(cuda_stream=0))
+    assert plan.last_launch_count() == 0
+    assert binding.load().fp2_window_prefill(plan.handle, *[None] * 9, 0, 0, None, None, None, None) == 1      # (a window all the same)
+    plan.close()
