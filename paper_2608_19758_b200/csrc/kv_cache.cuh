@@ -183,7 +183,7 @@ __device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq
 #pragma unroll
       for (int i = 0; i < kRows / 2; ++i) m = max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(max_abs_bf16x2(m, x[i].x), x[i].y), x[i].z), x[i].w);
       uint32_t amax = max(m & 0x7fffu, (m >> 16) & 0x7fffu);
-      if (__any_sync(0xffffffffu, amax >= 0x7f80u)) {      // an infinity, or nothing but NaN: the finite ones count
+      if (__any_sync(0xffffffffu, amax >= 0x7f80u)) {      // an infinity: the finite ones count (NaN has lost already)
         amax = 0;
 #pragma unroll
         for (int i = 0; i < kRows / 2; ++i) {

@@ -865,3 +865,20 @@ def test_decode_small_queries_on_large_keys(fmt, key, query):
     q = torch.from_numpy(st.rng.normal(0, 1.5, (6, 8, D)) * 2.0 ** query).bfloat16().cuda()
     out, lse = st.decode(q, [5, 1])
     check(st, q, [5, 1], out, lse, 0, 0)
+
+
+@pytest.mark.parametrize("page", [8, 16, 64])
+def test_append_a_page_of_nothing_but_nan(page):
+    """No finite magnitude in one head's page: the least scale, NaN codes; its neighbours as ever."""
+    st = Store(2, [0], 2, 2, page, capacity=[3 * page])
+    x = torch.from_numpy(st.rng.normal(0, 1, (3 * page, 2, D))).bfloat16()
+    x[page:2 * page, 1] = math.nan
+    x[2 * page:, 0] = math.nan
+    x[2 * page, 0, 3] = math.inf              # and one with an infinity among them
+    x = x.cuda()
+    want = plain_append(st, x, [3 * page], [3 * page], "k")
+    run_append(st, x, x, [3 * page], [3 * page])
+    assert same(st.dk, want[0]) and same(st.dks, want[1]) and same(st.dv, want[0])
+    one, two = int(st.pt[0, 1]), int(st.pt[0, 2])
+    assert float(st.dks[one, 1]) == 2.0 ** -100 and float(st.dks[two, 0]) == 2.0 ** -100
+    assert bool((st.dk[one, :, 1] & 0x7F == 0x7F).all()) and int(st.dk[two, 0, 0, 3]) == 0x7E
