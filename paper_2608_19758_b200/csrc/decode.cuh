@@ -741,7 +741,7 @@ decode_kernel(DecodeArgs A) {
     // waited for in its last step.)
     __syncwarp();
     if (more) {
-      if constexpr (NR <= 2) load_q(un);
+      load_q(un);
       pids_next = pids_un;
 #pragma unroll 1
       for (int k = 0; k < Cfg::kEarly; ++k) issue(un, k, k);
@@ -771,8 +771,6 @@ decode_kernel(DecodeArgs A) {
           *reinterpret_cast<float4*>(orow + piece(row, dim >> 2) * 4) = make_float4(o[n][t][v], o[n][t][2 + v], o[n][t + 1][v], o[n][t + 1][2 + v]);
         }
       }
-    if constexpr (NR > 2)                // (where O leaves no registers for them)
-      if (more) load_q(un);
     // Joins what the warps have put into shared memory.  place < 0: to out and lse; else to that row of the partial results.
     auto join = [&](long long place) {
       __syncthreads();

@@ -23,7 +23,7 @@ struct fp2_cache {
   int64_t ws_counters, ws_part_ml, ws_part_o, ws_bytes;
 };
 
-constexpr int kMaxDecodeTileRows = 32;
+constexpr int kMaxDecodeTileRows = 16;
 constexpr int64_t kMaxCacheTokens = 1ll << 30;   // positions and windows are 32-bit sums of two such
 
 static int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -36,7 +36,7 @@ static bool set_decode_attr() {
 }
 template <int FMT>
 static bool set_decode_attrs() {
-  return set_decode_attr<FMT, 1>() && set_decode_attr<FMT, 2>() && set_decode_attr<FMT, 4>();
+  return set_decode_attr<FMT, 1>() && set_decode_attr<FMT, 2>();
 }
 
 extern "C" fp2_status fp2_cache_create(const fp2_cache_params* p, fp2_cache** out) {
@@ -190,13 +190,14 @@ extern "C" fp2_status fp2_cache_expand(const fp2_cache* c, const void* k, const 
                 kExpandThreads, 0, stream, a);
 }
 
-// Packed rows of a tile by the rows that a sequence has on average: its pages are read once for all of them up to 32, and
-// below that no more than twice the rows there are is paid for.
+// Packed rows of a tile, 8 or 16, by the rows that a sequence has on average: its pages are copied once for all rows of a tile.
+// 32 sequences of 4096 tokens, heads 32 / 8, tiles of 8 / 16 rows, us: 4 rows BF16 86 / 88, head scales 54 / 57, page scales 57 / 69;
+// 8 rows 89 / 90, 55 / 58, 57 / 71; 12 rows 165 / 92, 98 / 60, 99 / 73; 20 rows 247 / 168, 147 / 103, 147 / 127.  Tiles of 32 rows, whose
+// accumulators do not fit the registers, took 236, 165 and 167 for 20 rows, and were behind for 32, 256 and 1024 rows too.
 template <int FMT>
 static fp2_status launch_decode(int64_t rows, int64_t grid, fp2_stream stream, const DecodeArgs& a) {
-  return rows <= 8    ? launch(decode_kernel<FMT, 1>, grid, kDecThreads, DecodeCfg<FMT, 1>::kSmemBytes, stream, a)
-         : rows <= 16 ? launch(decode_kernel<FMT, 2>, grid, kDecThreads, DecodeCfg<FMT, 2>::kSmemBytes, stream, a)
-                      : launch(decode_kernel<FMT, 4>, grid, kDecThreads, DecodeCfg<FMT, 4>::kSmemBytes, stream, a);
+  return rows <= 8 ? launch(decode_kernel<FMT, 1>, grid, kDecThreads, DecodeCfg<FMT, 1>::kSmemBytes, stream, a)
+                   : launch(decode_kernel<FMT, 2>, grid, kDecThreads, DecodeCfg<FMT, 2>::kSmemBytes, stream, a);
 }
 
 extern "C" fp2_status fp2_decode(const fp2_cache* c, const void* q, int64_t q_stride, const void* k, const void* v,
