@@ -36,7 +36,8 @@
 // Scales per page: ks multiplies the logits; vs enters P, in the exponent, so that P V needs none: y = x + log2 vs has the running
 // maximum of P, p = 2^(y - m).  The sum of the weights has a reference of its own, l = sum 2^(x - e): scales may lie 2^200 and more
 // apart (2^-100 is the writer's for a page of zeros), so what y hides can be the whole of l, and 2^-m is no unit for it.
-// (64 ragged sequences of 8-bit pages: 96.5 us with l taken back from P, p / vs, which loses weights and leaves fp32; 98.0 so.)
+// (64 ragged sequences of 8-bit pages: 95.6 us with l taken back from P, p / vs, which loses weights and leaves fp32; 94.0 so.  On
+// another card 97.5 / 102.)
 #pragma once
 #include <cuda_bf16.h>
 #include "common.cuh"
@@ -598,28 +599,27 @@ decode_kernel(DecodeArgs A) {
         a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 8));
         return fmaxf(a, __shfl_xor_sync(0xffffffffu, a, 16));
       };
-      auto move_e = [&](int n, int v) {  // l's own reference: to the maximum of x
-        float a = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < G; ++j) a = fmaxf(a, x[n][j / 2][(j & 1) * 2 + v]);
-        const float en = fmaxf(e[n][v], row_max(a));
-        l[n][v] *= en == e[n][v] ? 1.f : ex2(e[n][v] - en);
-        e[n][v] = en;
-      };
-      float my[NR][2];                   // this lane's maxima
+      // e moves with it, to the maximum of x, and by itself when a row has outgrown it by 30 (large weights on small values).
+      float my[NR][2], mx[OWN_E ? NR : 1][2];      // this lane's maxima
+      (void)mx;
       bool outgrown = false;
 #pragma unroll
       for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          float a = -INFINITY;
+          float a = -INFINITY, w = -INFINITY;
 #pragma unroll
           for (int j = 0; j < G; ++j) {
             const float y = x[n][j / 2][(j & 1) * 2 + v];
             a = fmaxf(a, OWN_E ? y + vlog[j] : y);
+            w = fmaxf(w, y);
           }
           my[n][v] = OWN_E ? a : a * cs[n][v];
           outgrown |= my[n][v] > m[n][v] + 14.f;
+          if constexpr (OWN_E) {
+            mx[n][v] = w;
+            outgrown |= w > e[n][v] + 30.f;
+          }
         }
       if (__any_sync(0xffffffffu, outgrown)) {
 #pragma unroll
@@ -629,8 +629,13 @@ decode_kernel(DecodeArgs A) {
             const float mn = fmaxf(m[n][v], row_max(my[n][v]) - 8.f);
             const float f = mn == m[n][v] ? 1.f : ex2(m[n][v] - mn);
             m[n][v] = mn;
-            if constexpr (OWN_E) move_e(n, v);
-            else l[n][v] *= f;
+            float g = f;
+            if constexpr (OWN_E) {
+              const float en = fmaxf(e[n][v], row_max(mx[n][v]));
+              g = en == e[n][v] ? 1.f : ex2(e[n][v] - en);
+              e[n][v] = en;
+            }
+            l[n][v] *= g;
 #pragma unroll
             for (int t = 0; t < 8; ++t) {
               o[n][t][v] *= f;
@@ -638,45 +643,17 @@ decode_kernel(DecodeArgs A) {
             }
           }
       }
-      if constexpr (OWN_E) {
-        // Weights against e, which a row may outgrow without outgrowing m (large weights on small values): then it moves first.
-        auto weights = [&](int n, int v) {
-          const float ref = e[n][v] == -INFINITY ? 0.f : e[n][v];
-          float sum = 0.f;
-#pragma unroll
-          for (int j = 0; j < G; ++j) sum += ex2(x[n][j / 2][(j & 1) * 2 + v] - ref);
-          return sum;
-        };
-        float add[NR][2];
-        bool large = false;
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            add[n][v] = weights(n, v);
-            large |= add[n][v] > 0x1p30f;
-          }
-        if (__any_sync(0xffffffffu, large)) {
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-              move_e(n, v);
-              add[n][v] = weights(n, v);
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) l[n][v] += add[n][v];
-      }
       uint32_t pb[NR][G], pl[FP8 ? 1 : NR][G];     // P^T: rows l4, tokens 8 j + 2 c, + 1
       (void)pl;
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
-        float ref[2];
+        float ref[2], ref_e[2];
 #pragma unroll
-        for (int v = 0; v < 2; ++v) ref[v] = m[n][v] == -INFINITY ? 0.f : m[n][v];
+        for (int v = 0; v < 2; ++v) {
+          ref[v] = m[n][v] == -INFINITY ? 0.f : m[n][v];
+          if constexpr (OWN_E) ref_e[v] = e[n][v] == -INFINITY ? 0.f : e[n][v];
+        }
+        (void)ref_e;
 #pragma unroll
         for (int j = 0; j < G; ++j) {
           float p[2];
@@ -685,6 +662,7 @@ decode_kernel(DecodeArgs A) {
             const float xj = x[n][j / 2][(j & 1) * 2 + v];
             if constexpr (OWN_E) {
               p[v] = ex2(xj + (vlog[j] - ref[v]));
+              l[n][v] += ex2(xj - ref_e[v]);
             } else {
               p[v] = ex2(fmaf(xj, cs[n][v], -ref[v]));
               l[n][v] += p[v];
