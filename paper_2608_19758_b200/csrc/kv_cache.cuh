@@ -94,6 +94,12 @@ __device__ __noinline__ float div_to_odd(float a, float s) {
   return __uint_as_float(__float_as_uint(q) | (rem < 0.f || rem > 0.f ? 1u : 0u));
 }
 
+// a * s likewise.  up: 2^64 where what was cut off could fall below the range of 32 bits, else 1
+__device__ __forceinline__ float mul_to_odd(float a, float s, float up) {
+  const float p = __fmul_rz(a, s), cut = fmaf(a, s * up, -(p * up));
+  return __uint_as_float(__float_as_uint(p) | (cut < 0.f || cut > 0.f ? 1u : 0u));
+}
+
 // New tokens of one sequence: rows c0 .. c1 - 1, the sequence L tokens long with them
 struct AppendSeq {
   int b, c0, c1, L;
@@ -205,7 +211,8 @@ __device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq
       if (!active) continue;
       scale = fmaxf(page_scale_for(amax), before);
       if (keeps && scale > before) {   // earlier rows of the page to the larger scale (a power of two then)
-        const float inv = 1.0f / scale;
+        const float inv = 1.0f / scale, up = before < 0x1p-60f ? 0x1p64f : 1.f;   // (rounded once: by e4m3)
+        auto again = [&](float code) { return mul_to_odd(code, before, up) * inv; };
 #pragma unroll 1
         for (int i = 0; i < kRows / 2; ++i) {
           const int row = row0 + 2 * i;
@@ -217,7 +224,7 @@ __device__ __forceinline__ void append_page(const AppendArgs& A, const AppendSeq
           for (int k = 0; k < 2; ++k) {
             const uint32_t w = k ? old.y : old.x;
             const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(w & 0xffffu)), c = f16x2_to_float2(e4m3x2_to_f16x2(w >> 16));
-            o[k] = pack_e4m3x2(a.x * before * inv, a.y * before * inv) | pack_e4m3x2(c.x * before * inv, c.y * before * inv) << 16;
+            o[k] = pack_e4m3x2(again(a.x), again(a.y)) | pack_e4m3x2(again(c.x), again(c.y)) << 16;
           }
           *p = make_uint2(o[0], o[1]);
         }
@@ -330,12 +337,7 @@ __device__ __forceinline__ bool rounds_twice(float s) {
   for (int c = 8; c < 16; ++c) bad |= (__float_as_uint(s * (c * 0x1p-7f)) & 0xffffu) == 0x8000u;
   return bad && !exact_products(s);
 }
-// Then the product is rounded to odd (see div_to_odd; up: 2^64 where what was cut off could fall below the range of 32 bits), which
-// leaves the one rounding to BF16.  Two codes; a call, to leave its registers to the common path.
-__device__ __forceinline__ float mul_to_odd(float a, float s, float up) {
-  const float p = __fmul_rz(a, s), cut = fmaf(a, s * up, -(p * up));
-  return __uint_as_float(__float_as_uint(p) | (cut < 0.f || cut > 0.f ? 1u : 0u));
-}
+// Then the product is rounded to odd, which leaves the one rounding to BF16.  Two codes; a call, to leave its registers to the common path.
 __device__ __noinline__ uint32_t widen_rounding_once(uint32_t codes, float s) {
   const float2 a = f16x2_to_float2(e4m3x2_to_f16x2(codes & 0xffffu));
   const float up = s < 0x1p-60f ? 0x1p64f : 1.f;

@@ -882,3 +882,28 @@ def test_append_a_page_of_nothing_but_nan(page):
     one, two = int(st.pt[0, 1]), int(st.pt[0, 2])
     assert float(st.dks[one, 1]) == 2.0 ** -100 and float(st.dks[two, 0]) == 2.0 ** -100
     assert bool((st.dk[one, :, 1] & 0x7F == 0x7F).all()) and int(st.dk[two, 0, 0, 3]) == 0x7E
+
+
+def test_append_rounds_what_a_page_holds_once():
+    """A page under a caller's scale grows: its earlier tokens go to the e4m3 values nearest to code * scale / new scale, the product
+    (28 bits) not rounded to 32 bits on the way."""
+    rng = np.random.default_rng(6)
+    hkv = 128
+    pos = e4m3_values()[:127].numpy()
+    code = np.arange(8, 16)[rng.integers(0, 8, hkv)] / 8.0                    # significands of the codes
+    middle = (np.arange(8, 16)[rng.integers(0, 8, hkv)] + 0.5) / 8.0
+    s = (middle / code).astype(np.float32)
+    s = np.nextafter(s, np.where(np.arange(hkv) % 2 == 0, np.float32(0), np.float32(9))).astype(np.float32)
+    st = Store(2, [5], hkv, hkv, 16, capacity=[6])
+    pid = int(st.pt[0, 0])
+    old = torch.from_numpy(rng.integers(0, 127, (5, hkv, D)).astype(np.uint8) + (128 * rng.integers(0, 2, (5, hkv, D))).astype(np.uint8))
+    old[0] = torch.arange(D, dtype=torch.uint8)[None].clamp(max=126)          # every code
+    for x, sc in ((st.dk, st.dks), (st.dv, st.dvs)):
+        x[pid, :5] = old.cuda()
+        sc[pid] = torch.from_numpy(s).cuda()
+    new = torch.full((1, hkv, D), 448.0 * 4, dtype=torch.bfloat16, device="cuda")      # needs a scale of 4: s is below 2
+    run_append(st, new, new, [6], [1])
+    value = old.view(E4M3).double().numpy() * s.astype(np.float64)[None, :, None] / 4
+    want = torch.from_numpy(nearest_e4m3(value))
+    for x, sc in ((st.dk, st.dks), (st.dv, st.dvs)):
+        assert torch.equal(x[pid, :5].cpu(), want) and bool((sc[pid] == 4.0).all()) and bool((x[pid, 5] == 0x7E).all())
