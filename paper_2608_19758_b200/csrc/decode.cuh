@@ -18,8 +18,8 @@
 // write zeros without reading, so nothing that stands in a hidden place reaches the sums.  192 KB of an SM take part.
 // (By TMA, a box per page and operand, lanes in turn: everything 4 to 6 % slower.)
 //
-// Measured, whole calls: 64 sequences of 4096 tokens, 8 KV heads, 168 us in BF16 (6.4 TB/s, 0.98 of the copy rate), 100 us in 8 bits
-// (5.4 TB/s, 0.82; 37 sequences of 8192 tokens, a whole unit per CTA, 6.2 TB/s: the rest is the units' ends, 2.5 parts per CTA);
+// Measured, whole calls: 64 sequences of 4096 tokens, 8 KV heads, 168 us in BF16 (6.4 TB/s, 0.98 of the copy rate), 100 to 105 us in 8 bits
+// (by card; 5.4 TB/s, 0.82; 37 sequences of 8192 tokens, a whole unit per CTA, 6.2 TB/s: the rest is the units' ends, 2.5 parts per CTA);
 // 131072 tokens of 4 heads 52 us in BF16, of which 41 are the bytes, 5 the start and 5 the joining of 74 parts per head.
 //
 // S^T = K Q^T and O^T += V^T P^T are m16n8k16 MMAs of a warp with the tokens (then the dims) as the long side and 8 packed

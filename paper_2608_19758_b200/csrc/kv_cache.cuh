@@ -66,8 +66,8 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // of e4m3 out each), eight rows in flight per lane.  A CTA looks its page up once and goes over the page's heads (or, when there
 // are few pages, `split` CTAs share them): what a warp does is wait, for the lengths, then for tokens and page id together, so it
 // should not wait again for each head.  41392 tokens, 8 heads, 64 a page: 59.6 us with a CTA and its look-ups for every 32 KB,
-// 47.9 so (5.3 TB/s, 0.81 of the copy rate); 256 sequences of one token 9.9 / 6.8 us.  Bound by memory for prompts (2 bytes read and 1 written per element), by launch and load
-// latency for single tokens.
+// 45.7 so (5.6 TB/s, 0.85 of the copy rate); 256 sequences of one token 9.9 / 6.7 us.  Bound by memory for prompts (2 bytes read and 1
+// written per element), by launch and load latency for single tokens.
 constexpr int kAppendThreads = 256;
 
 struct AppendArgs {
