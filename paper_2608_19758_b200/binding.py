@@ -170,12 +170,10 @@ class Plan:
         a, b, c = C.c_int64(), C.c_int64(), C.c_int64()
         _check(lib.fp2_plan_sizes(h, C.byref(a), C.byref(b), C.byref(c)), "fp2_plan_sizes")
         self.num_segments, self.idx_capacity, self.workspace_bytes = a.value, b.value, c.value
-        self._device = torch.cuda.current_device() if torch.cuda.is_available() else -1
         p = self.params
-        self._fp8 = p.dtype != 0
-        self._kinds = _E4M3 if self._fp8 else _BF16
-        self._q_size, self._pool_size = p.total_q * p.num_q_heads * 128, p.num_pages * p.page_size * p.num_kv_heads * 128
-        self._pt_shape, self._lse_shape = (p.num_seqs, p.max_pages_per_seq), (p.num_q_heads, p.total_q)
+        self._window_sizes = (p.total_q * p.num_q_heads * 128, p.num_pages * p.page_size * p.num_kv_heads * 128,
+                              (p.num_seqs, p.max_pages_per_seq), (p.num_q_heads, p.total_q), p.num_q_heads if p.dtype else 0,
+                              p.num_kv_heads, _E4M3 if p.dtype else _BF16)
 
     def segment(self, seg: int) -> dict:
         out = (C.c_int32 * 10)()
@@ -252,33 +250,53 @@ def fp2_dense_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q,
            "fp2_dense_prefill")
 
 
+def _check_window(plan, q, k_cache, v_cache, page_table, q_scale, k_scale, v_scale, out, lse, workspace):
+    """What fp2_window_prefill reads and writes must be what the plan takes its address for; more elements may follow behind.  (Looked
+    at in one expression, which is a microsecond, and again one by one only to say what is wrong.)"""
+    q_size, pool, pt_shape, lse_shape, heads, kv_heads, kinds = plan._window_sizes
+    dev = torch.cuda.current_device() if torch.cuda.is_initialized() or torch.cuda.is_available() else -1
+    try:
+        fits = (q.dtype in kinds and q.numel() >= q_size and q.get_device() == dev and q.is_contiguous() and
+                k_cache.dtype in kinds and k_cache.numel() >= pool and k_cache.get_device() == dev and k_cache.is_contiguous() and
+                v_cache.dtype in kinds and v_cache.numel() >= pool and v_cache.get_device() == dev and v_cache.is_contiguous() and
+                out.dtype is torch.bfloat16 and out.numel() >= q_size and out.get_device() == dev and out.is_contiguous() and
+                page_table.dtype is torch.int32 and page_table.shape == pt_shape and page_table.get_device() == dev and
+                page_table.is_contiguous() and workspace.nbytes >= plan.workspace_bytes and workspace.get_device() == dev and
+                (lse is None or lse.dtype is torch.float32 and lse.shape == lse_shape and lse.get_device() == dev and
+                 lse.is_contiguous()))
+        if heads:                       # FP8
+            fits = (fits and q_scale.dtype is torch.float32 and q_scale.numel() >= heads and q_scale.get_device() == dev and
+                    q_scale.is_contiguous() and k_scale.dtype is torch.float32 and k_scale.numel() >= kv_heads and
+                    k_scale.get_device() == dev and k_scale.is_contiguous() and v_scale.dtype is torch.float32 and
+                    v_scale.numel() >= kv_heads and v_scale.get_device() == dev and v_scale.is_contiguous())
+    except AttributeError:              # None
+        fits = False
+    if fits:
+        return
+    where = "fp2_window_prefill"
+    _room(where, dev, q, kinds, q_size)
+    _room(where, dev, k_cache, kinds, pool)
+    _room(where, dev, v_cache, kinds, pool)
+    _room(where, dev, out, _BF16, q_size)
+    _room(where, dev, page_table, _I32, pt_shape[0] * pt_shape[1])
+    if page_table.dim() > 1 and page_table.shape[-1] != pt_shape[1]:           # (more sequences may follow, rows be no longer)
+        _want(where, dev, page_table, _I32, pt_shape)
+    if lse is not None:
+        _want(where, dev, lse, _F32, lse_shape)
+    for scale, n in ((q_scale, heads), (k_scale, kv_heads), (v_scale, kv_heads)) if heads else ():
+        _room(where, dev, scale, _F32, n)
+    if workspace is None or workspace.nbytes < plan.workspace_bytes or workspace.get_device() != dev:
+        raise Fp2Error(1, f"{where}: workspace too small or not on device {dev}")
+
+
 def fp2_window_prefill(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale, v_scale,
                        window_tokens: int, sink_tokens: int, out, lse, workspace, stream=None):
     """Causal attention with a sliding window of `window_tokens` and the first `sink_tokens` tokens always visible."""
-    where, dev, kinds = "fp2_window_prefill", plan._device, plan._kinds
-    if not (q.dtype in kinds and q.numel() >= plan._q_size and q.get_device() == dev and q.is_contiguous() and
-            k_cache.dtype in kinds and k_cache.numel() >= plan._pool_size and k_cache.get_device() == dev and k_cache.is_contiguous() and
-            v_cache.dtype in kinds and v_cache.numel() >= plan._pool_size and v_cache.get_device() == dev and v_cache.is_contiguous() and
-            out.dtype is torch.bfloat16 and out.numel() >= plan._q_size and out.get_device() == dev and out.is_contiguous()):
-        _room(where, dev, q, kinds, plan._q_size)
-        _room(where, dev, k_cache, kinds, plan._pool_size)
-        _room(where, dev, v_cache, kinds, plan._pool_size)
-        _room(where, dev, out, _BF16, plan._q_size)
-    if not (page_table.dtype is torch.int32 and page_table.shape == plan._pt_shape and page_table.get_device() == dev and
-            page_table.is_contiguous()):
-        _want(where, dev, page_table, _I32, plan._pt_shape)
-    if lse is not None and not (lse.dtype is torch.float32 and lse.shape == plan._lse_shape and lse.get_device() == dev and
-                                lse.is_contiguous()):
-        _want(where, dev, lse, _F32, plan._lse_shape)
-    if plan._fp8:
-        _room(where, dev, q_scale, _F32, plan.params.num_q_heads)
-        _room(where, dev, k_scale, _F32, plan.params.num_kv_heads)
-        _room(where, dev, v_scale, _F32, plan.params.num_kv_heads)
-    if workspace.nbytes < plan.workspace_bytes or workspace.get_device() != dev:
-        raise Fp2Error(1, f"{where}: workspace too small or not on device {dev}")
+    _check_window(plan, q, k_cache, v_cache, page_table, q_scale, k_scale, v_scale, out, lse, workspace)
     _check(load().fp2_window_prefill(plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
                                      _ptr(cu_seqlens_q), _ptr(seqlens_k), _ptr(q_scale), _ptr(k_scale), _ptr(v_scale),
-                                     window_tokens, sink_tokens, _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)), where)
+                                     window_tokens, sink_tokens, _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)),
+           "fp2_window_prefill")
 
 
 def fp2_dense_prefill_static(plan: Plan, q, k_cache, v_cache, page_table, cu_seqlens_q, seqlens_k, q_scale, k_scale,

@@ -207,13 +207,14 @@ def test_window_prefill_refuses_tensors_that_are_not_what_the_address_is_taken_f
            ("page_table", pt.long()), ("page_table", torch.zeros(2, 40, dtype=torch.int32)), ("page_table", torch.zeros(2, 40, dtype=torch.int32)[:, :32]),
            ("out", torch.zeros(300, 16, 128, dtype=torch.bfloat16)[:, :8]), ("out", out.float()), ("out", out[1:]), ("lse", lse.T), ("lse", torch.zeros(8, 400)),
            ("lse", lse.double()), ("workspace", good["workspace"][:64])]
+    bad += [(name, None) for name in ("q", "k_cache", "v_cache", "page_table", "out", "workspace")]
     if fp8:
         bad += [("q_scale", None), ("q_scale", torch.ones(7)), ("k_scale", torch.ones(2).double()), ("v_scale", torch.ones(4)[::2])]
     for name, value in bad:
         with pytest.raises(binding.Fp2Error) as e:
             binding.fp2_window_prefill(plan, **{**good, name: value})
         assert e.value.code == 1, (name, value.shape if value is not None else None)
-    more = dict(q=torch.zeros(400, 8, 128, dtype=kind), out=torch.zeros(400, 8, 128, dtype=torch.bfloat16), k_cache=torch.zeros(70, 16, 2, 128, dtype=kind))
+    more = dict(page_table=torch.zeros(5, 32, dtype=torch.int32), q=torch.zeros(400, 8, 128, dtype=kind), out=torch.zeros(400, 8, 128, dtype=torch.bfloat16), k_cache=torch.zeros(70, 16, 2, 128, dtype=kind))
     for kw in ({}, more, dict(lse=None), dict(k_cache=k.view(-1, 2, 128))):
         with pytest.raises(binding.Fp2Error) as e:
             binding.fp2_window_prefill(plan, **{**good, **kw})
